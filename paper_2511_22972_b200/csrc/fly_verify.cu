@@ -11,6 +11,7 @@
 
 #include <cudaTypedefs.h>
 
+#include "device_guard.h"
 #include "fly_common.cuh"
 #include "host_span.h"
 #include "lmhead_kernel.cuh"
@@ -27,20 +28,6 @@ constexpr int kReduceUnroll = 4;
 constexpr int64_t kMinBlockBytes = 16384;   // a block that gets less than this is all fixed cost
 constexpr int kMaxK = 63;
 constexpr size_t kDirectBytes = 5 << 20;    // host logits up to this size are read in place (fly_verify_run_host, with the figures)
-
-struct DeviceGuard {
-  int prev = -1;
-  bool ok = true;
-  explicit DeviceGuard(int dev) {
-    if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-    if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
-    want = dev;
-  }
-  ~DeviceGuard() {
-    if (ok && prev != want) cudaSetDevice(prev);
-  }
-  int want = -1;
-};
 
 }  // namespace
 
@@ -256,19 +243,6 @@ FlatPlan plan_flat(int sm_count, int64_t rows, int64_t n, int elem_bytes, bool v
   const int64_t most = s > 0 ? s : (n + pl.Q - 1) / pl.Q + 1;
   pl.slots = (int)(most < cap ? most : cap);
   return pl;
-}
-
-void fill_launch(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* attr, unsigned grid, unsigned block, cudaStream_t st,
-                 bool programmatic) {
-  memset(cfg, 0, sizeof(*cfg));
-  cfg->gridDim = dim3(grid);
-  cfg->blockDim = dim3(block);
-  cfg->dynamicSmemBytes = 0;
-  cfg->stream = st;
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = programmatic ? 1 : 0;
-  cfg->attrs = attr;
-  cfg->numAttrs = 1;
 }
 
 // Shared memory of the row reduction's cp.async rings (vector path) and of the slice that each warp keeps, per block.

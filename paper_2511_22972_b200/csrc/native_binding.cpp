@@ -20,6 +20,7 @@
 #include <c10/core/DeviceGuard.h>
 #include <c10/core/impl/LocalDispatchKeySet.h>
 
+#include "fly_cache.h"
 #include "fly_verify.h"
 
 namespace {
@@ -31,6 +32,9 @@ struct Api {
   decltype(&fly_verify_run_partials) run_partials;
   decltype(&fly_verify_run_static) run_static;
   decltype(&fly_pld_draft) pld_draft;
+  decltype(&fly_cache_append) cache_append;
+  decltype(&fly_cache_read) cache_read;
+  decltype(&fly_attention_run) attention_run;
 } api;
 
 // Address of a tensor's storage; None is a null pointer.  Anything else that has data_ptr() is asked for it.
@@ -363,6 +367,127 @@ PyObject* py_pld_draft(PyObject*, PyObject* const* v, Py_ssize_t n) {
                        THPVariable_Wrap(ngram));
 }
 
+// init_cache(cache_append, cache_read, attention_run)
+PyObject* py_init_cache(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (!enough(n, 3)) return nullptr;
+  void* p[3];
+  for (int i = 0; i < 3; ++i) {
+    p[i] = PyLong_AsVoidPtr(v[i]);
+    if (!p[i] && PyErr_Occurred()) return nullptr;
+  }
+  api.cache_append = (decltype(api.cache_append))p[0];
+  api.cache_read = (decltype(api.cache_read))p[1];
+  api.attention_run = (decltype(api.attention_run))p[2];
+  Py_RETURN_NONE;
+}
+
+bool value_error(bool ok, const char* what) {
+  if (!ok) PyErr_SetString(PyExc_ValueError, what);
+  return ok;
+}
+
+// A bf16 tensor [B, n, heads, head_dim] on the cache's device; B < 0: its B and n are taken.
+bool rows(PyObject* o, const fly_cache_t* c, int64_t heads, int64_t* B, int64_t* n, fly_rows_t* r) {
+  if (!value_error(THPVariable_Check(o), "rows are tensors")) return false;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!value_error(t.dim() == 4 && t.scalar_type() == at::kBFloat16, "rows are [B, n, heads, head_dim] bfloat16")) return false;
+  if (*B < 0) {
+    *B = t.size(0);
+    *n = t.size(1);
+  }
+  if (!value_error(t.size(0) == *B && t.size(1) == *n && t.size(2) == heads && t.size(3) == c->head_dim, "rows are [B, n, heads, head_dim], alike and as the cache has them") ||
+      !value_error(t.stride(3) == 1, "rows have a contiguous head_dim") ||
+      !value_error(t.is_cuda() && t.get_device() == c->device, "rows are on the cache's device") ||
+      !value_error(*B <= 0x7fffffff && *n <= 0x7fffffff, "B and n are below 2^31"))
+    return false;
+  *r = {t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)};
+  return true;
+}
+
+// None, or a contiguous tensor of so many values of this type on the cache's device.
+bool values(PyObject* o, const fly_cache_t* c, at::ScalarType type, int64_t count, const char* what, void** p) {
+  *p = nullptr;
+  if (o == Py_None) return true;
+  if (!value_error(THPVariable_Check(o), what)) return false;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!value_error(t.scalar_type() == type && t.numel() == count && t.is_contiguous() && t.is_cuda() && t.get_device() == c->device, what)) return false;
+  *p = t.data_ptr();
+  return true;
+}
+
+// cache_append(cache, k, v, counts, row_flags, stream)
+PyObject* py_cache_append(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (!enough(n, 6)) return nullptr;
+  const fly_cache_t* c = (const fly_cache_t*)PyLong_AsVoidPtr(v[0]);
+  if (!c) return PyErr_Occurred() ? nullptr : status(FLY_ERR_INVALID_ARG);
+  int64_t B = -1, m = -1;
+  fly_rows_t k, w;
+  void *counts, *flags;
+  if (!rows(v[1], c, c->kv_heads, &B, &m, &k) || !rows(v[2], c, c->kv_heads, &B, &m, &w) ||
+      !values(v[3], c, at::kInt, B, "counts is [B] int32 on the cache's device", &counts) ||
+      !values(v[4], c, at::kInt, B * m, "row_flags is [B, n] int32 on the cache's device", &flags))
+    return nullptr;
+  void* stream = PyLong_AsVoidPtr(v[5]);
+  if (PyErr_Occurred()) return nullptr;
+  fly_status_t s;
+  {
+    Unlocked unlocked;
+    s = api.cache_append(c, (int32_t)B, (int32_t)m, &k, &w, (const int32_t*)counts, (uint32_t*)flags, stream);
+  }
+  return status(s);
+}
+
+// cache_read(cache, k_out, v_out, starts, stream)
+PyObject* py_cache_read(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (!enough(n, 5)) return nullptr;
+  const fly_cache_t* c = (const fly_cache_t*)PyLong_AsVoidPtr(v[0]);
+  if (!c) return PyErr_Occurred() ? nullptr : status(FLY_ERR_INVALID_ARG);
+  int64_t B = -1, m = -1;
+  fly_rows_t k, w;
+  void* starts;
+  if (!rows(v[1], c, c->kv_heads, &B, &m, &k) || !rows(v[2], c, c->kv_heads, &B, &m, &w) ||
+      !values(v[3], c, at::kInt, B, "starts is [B] int32 on the cache's device", &starts))
+    return nullptr;
+  void* stream = PyLong_AsVoidPtr(v[4]);
+  if (PyErr_Occurred()) return nullptr;
+  fly_status_t s;
+  {
+    Unlocked unlocked;
+    s = api.cache_read(c, (int32_t)B, (int32_t)m, (const int32_t*)starts, &k, &w, stream);
+  }
+  return status(s);
+}
+
+// attention_run(handle, cache, heads, q, out, window, sinks, scale, counts, lse, stream)
+PyObject* py_attention_run(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (!enough(n, 11)) return nullptr;
+  fly_attention_t* h = (fly_attention_t*)PyLong_AsVoidPtr(v[0]);
+  if (!h && PyErr_Occurred()) return nullptr;
+  const fly_cache_t* c = (const fly_cache_t*)PyLong_AsVoidPtr(v[1]);
+  if (!c) return PyErr_Occurred() ? nullptr : status(FLY_ERR_INVALID_ARG);
+  int64_t B = -1, m = -1;
+  long long heads, window, sinks;
+  fly_attention_args_t a = {};
+  if (!integer(v[2], &heads) || !rows(v[3], c, heads, &B, &m, &a.q) || !rows(v[4], c, heads, &B, &m, &a.out) || !integer(v[5], &window) ||
+      !integer(v[6], &sinks) || !number(v[7], &a.scale) ||
+      !value_error(window >= 0 && window <= 0x7fffffff && sinks >= 0 && sinks <= 0x7fffffff, "window and sinks are from 0 to 2^31 - 1") ||
+      !values(v[8], c, at::kInt, B, "counts is [B] int32 on the cache's device", (void**)&a.counts) ||
+      !values(v[9], c, at::kFloat, B * m * heads, "lse is [B, n, heads] float32 on the cache's device", (void**)&a.lse))
+    return nullptr;
+  void* stream = PyLong_AsVoidPtr(v[10]);
+  if (PyErr_Occurred()) return nullptr;
+  a.B = (int32_t)B;
+  a.n = (int32_t)m;
+  a.window = (int32_t)window;
+  a.sinks = (int32_t)sinks;
+  fly_status_t s;
+  {
+    Unlocked unlocked;
+    s = api.attention_run(h, c, &a, stream);
+  }
+  return status(s);
+}
+
 // A C++ exception must not leave a function that Python calls.
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject* self, PyObject* const* v, Py_ssize_t n) {
@@ -373,7 +498,8 @@ PyObject* guarded(PyObject* self, PyObject* const* v, Py_ssize_t n) {
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))guarded<py_##name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(init),         FAST(fill), FAST(verify),       FAST(verify_fused), FAST(reduce_shard),
-                         FAST(run_partials), FAST(run),  FAST(run_static), FAST(pld_draft),    {nullptr, nullptr, 0, nullptr}};
+                         FAST(run_partials), FAST(run),  FAST(run_static), FAST(pld_draft),    
+                         FAST(init_cache),   FAST(cache_append), FAST(cache_read), FAST(attention_run), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Native argument marshalling of the C ABI.", -1, methods};
 
 }  // namespace
