@@ -123,6 +123,16 @@ typedef struct {
 fly_status_t fly_attention_run(fly_attention_t* handle, const fly_cache_t* cache, const fly_attention_args_t* args,
                                void* cuda_stream);
 
+/* The kernel waits on hardware barriers (loads, tensor cores); every such wait is bounded (200 ms).  If one runs out, the kernel
+ * records it and returns without hanging, and rows that it could not form are NaN (out and lse).  This call synchronises
+ * `cuda_stream` and returns FLY_ERR_TIMEOUT if that happened since the last call (the record is cleared), else FLY_OK.  While
+ * a record is pending, every further step of the handle comes back as NaN. */
+fly_status_t fly_attention_device_status(fly_attention_t* handle, void* cuda_stream);
+
+/* Self-test of that mechanism, safe to run anywhere: enqueues a one-thread kernel that waits, with a 2 ms limit, on a barrier
+ * that nothing completes.  It gives up and returns normally, and fly_attention_device_status reports FLY_ERR_TIMEOUT. */
+fly_status_t fly_attention_selftest_wait(fly_attention_t* handle, void* cuda_stream);
+
 /* Number of kernels the last fly_attention_run enqueued, and the cudaError_t of the last failed CUDA call (0 if none). */
 int32_t fly_attention_last_launch_count(const fly_attention_t* handle);
 int32_t fly_attention_last_cuda_error(const fly_attention_t* handle);

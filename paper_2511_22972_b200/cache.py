@@ -18,7 +18,7 @@ FLY_CACHE_BF16, FLY_CACHE_E4M3 = 0, 1
 FLAG_NOT_WRITTEN = 32
 
 EXPORTS = ("fly_cache_append", "fly_cache_read", "fly_attention_create", "fly_attention_destroy", "fly_attention_run",
-           "fly_attention_last_launch_count", "fly_attention_last_cuda_error")
+           "fly_attention_device_status", "fly_attention_selftest_wait", "fly_attention_last_launch_count", "fly_attention_last_cuda_error")
 
 
 class fly_cache_t(C.Structure):
@@ -59,6 +59,8 @@ def lib() -> C.CDLL:
     L.fly_attention_create.argtypes = [P(fly_attention_config_t), P(C.c_void_p)]
     L.fly_attention_destroy.argtypes = [C.c_void_p]
     L.fly_attention_run.argtypes = [C.c_void_p, P(fly_cache_t), P(fly_attention_args_t), C.c_void_p]
+    L.fly_attention_device_status.argtypes = [C.c_void_p, C.c_void_p]
+    L.fly_attention_selftest_wait.argtypes = [C.c_void_p, C.c_void_p]
     L.fly_attention_last_launch_count.argtypes = [C.c_void_p]
     L.fly_attention_last_cuda_error.argtypes = [C.c_void_p]
     for name in EXPORTS:
@@ -154,6 +156,14 @@ class ChunkAttention:
     @property
     def last_launch_count(self) -> int:
         return int(lib().fly_attention_last_launch_count(self._h))
+
+    def device_status(self, stream: int = 0) -> int:
+        """fly_attention_device_status: synchronises the stream; FLY_OK or FLY_ERR_TIMEOUT."""
+        return int(lib().fly_attention_device_status(self._h, C.c_void_p(stream)))
+
+    def selftest_wait(self, stream: int = 0) -> int:
+        """fly_attention_selftest_wait: makes one bounded device-side wait run out on purpose (no fault)."""
+        return int(lib().fly_attention_selftest_wait(self._h, C.c_void_p(stream)))
 
     def run(self, cache: PagedCache, q, out, window: int = 0, sinks: int = 0, scale: float = 0.0, counts=None, lse=None, stream: int = 0):
         """fly_attention_run: q [B, n, heads, head_dim] bf16 -> out, alike; the chunk has been appended behind cache.lengths.

@@ -3,7 +3,10 @@
 #include "fly_cache.h"
 
 #include <cmath>
+#include <initializer_list>
 #include <new>
+
+#include <cudaTypedefs.h>
 
 #include "attention_kernel.cuh"
 #include "cache_kernel.cuh"
@@ -11,6 +14,12 @@
 
 struct fly_attention {
   fly_attention_config_t cfg;
+  int sm_count = 148;
+  float* part_o = nullptr;  // one block: parts of items | their references and sums | how the ranges begin | status word
+  float2* part_ml = nullptr;
+  int* desc = nullptr;
+  int* status = nullptr;
+  PFN_cuTensorMapEncodeTiled encode_tiled = nullptr;
   int last_launches = 0;
   int last_cuda_error = 0;
 };
@@ -18,6 +27,9 @@ struct fly_attention {
 namespace {
 
 namespace K = fly::cache;
+namespace A = fly::attn;
+
+constexpr int kMaxTokens = 1 << 28;  // of a chunk: a position and a chunk's end are int32
 
 bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
@@ -34,7 +46,7 @@ fly_status_t check_cache(const fly_cache_t* c, int32_t B, int32_t n) {
   if (c->page_stride < 0 || c->token_stride < 0 || c->head_stride < 0) return FLY_ERR_INVALID_ARG;
   if (c->head_dim != 64 && c->head_dim != 128) return FLY_ERR_UNSUPPORTED;
   if (c->page_size < 8 || c->page_size > 65536 || (c->page_size & (c->page_size - 1)) != 0) return FLY_ERR_UNSUPPORTED;
-  if ((int64_t)c->max_pages * c->page_size > (int64_t)1 << 30 || n > 1 << 30) return FLY_ERR_UNSUPPORTED;
+  if ((int64_t)c->max_pages * c->page_size > (int64_t)1 << 30 || n > kMaxTokens) return FLY_ERR_UNSUPPORTED;
   const int64_t unit = e4m3 ? 16 : 8;  // elements in 16 bytes
   if (!aligned(c->k_pages, 16) || !aligned(c->v_pages, 16) || (e4m3 && (!aligned(c->k_scales, 8) || !aligned(c->v_scales, 8))))
     return FLY_ERR_UNSUPPORTED;
@@ -85,6 +97,51 @@ bool row_grid(const fly_cache_t* c, int32_t B, int32_t n, dim3* grid) {
   return true;
 }
 
+template <int D, bool E4M3, bool PAIR>
+cudaError_t set_attrs() {
+  return cudaFuncSetAttribute(A::attention_kernel<D, E4M3, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, A::Shape<D, E4M3, PAIR>::kSmem);
+}
+cudaError_t set_attention_attrs() {
+  cudaError_t e = cudaSuccess;
+  for (cudaError_t x : {set_attrs<64, false, false>(), set_attrs<64, false, true>(), set_attrs<64, true, false>(), set_attrs<64, true, true>(),
+                        set_attrs<128, false, false>(), set_attrs<128, false, true>(), set_attrs<128, true, false>(), set_attrs<128, true, true>()})
+    if (e == cudaSuccess) e = x;
+  return e;
+}
+
+// A four-dimensional tensor of bf16 (128-byte swizzle) or of codes (as they lie); dims[0] contiguous, strides in elements.
+bool encode(fly_attention* h, CUtensorMap* map, const void* data, bool codes, const int64_t* dims, const int64_t* strides, const int* box) {
+  const int esz = codes ? 1 : 2;
+  cuuint64_t d[4], s[3];
+  cuuint32_t b[4], one[4] = {1, 1, 1, 1};
+  for (int i = 0; i < 4; ++i) {
+    d[i] = (cuuint64_t)dims[i];
+    b[i] = (cuuint32_t)box[i];
+  }
+  for (int i = 0; i < 3; ++i) s[i] = (cuuint64_t)(dims[i + 1] > 1 ? strides[i] : dims[0]) * esz;  // (of a dimension of one entry: anything)
+  return h->encode_tiled(map, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(data), d, s, b, one,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, codes ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, bool E4M3, bool PAIR>
+cudaError_t launch(fly_attention* h, const CUtensorMap* maps, const A::Params& p, cudaStream_t st) {
+  using S = A::Shape<D, E4M3, PAIR>;
+  cudaLaunchConfig_t cfg;
+  cudaLaunchAttribute attr[1];
+  fill_launch(&cfg, attr, (unsigned)h->sm_count, S::kThreads, st, true);
+  cfg.dynamicSmemBytes = S::kSmem;
+  cudaError_t e = cudaLaunchKernelEx(&cfg, A::attention_kernel<D, E4M3, PAIR>, maps[0], maps[1], maps[2], p);
+  if (e != cudaSuccess || h->sm_count < 2) return e;
+  h->last_launches++;
+  fill_launch(&cfg, attr, (unsigned)h->sm_count - 1, A::kCombineThreads, st, true);
+  const int used = PAIR ? S::kItemRows : p.tpt * p.group;
+  cfg.gridDim.y = (unsigned)((used + A::kCombineThreads / 32 - 1) / (A::kCombineThreads / 32));
+  e = cudaLaunchKernelEx(&cfg, A::attention_combine_kernel<D>, p, (int)S::kItemRows);
+  if (e == cudaSuccess) h->last_launches++;
+  return e;
+}
+
 }  // namespace
 
 extern "C" {
@@ -131,15 +188,45 @@ fly_status_t fly_attention_create(const fly_attention_config_t* c, fly_attention
   if (!c || !out) return FLY_ERR_INVALID_ARG;
   if (c->device < 0 || c->max_batch < 1 || c->max_tokens < 1 || c->kv_heads < 1 || c->heads < 1 || c->heads % c->kv_heads != 0 || c->head_dim < 1)
     return FLY_ERR_INVALID_ARG;
-  if ((c->head_dim != 64 && c->head_dim != 128) || c->heads / c->kv_heads > 128) return FLY_ERR_UNSUPPORTED;
+  if ((c->head_dim != 64 && c->head_dim != 128) || c->heads / c->kv_heads > A::kTileRows || c->max_tokens > kMaxTokens) return FLY_ERR_UNSUPPORTED;
   fly_attention* h = new (std::nothrow) fly_attention();
   if (!h) return FLY_ERR_INVALID_ARG;
   h->cfg = *c;
+  DeviceGuard g(c->device);
+  cudaStream_t st = nullptr;
+  cudaError_t e = g.ok ? cudaDeviceGetAttribute(&h->sm_count, cudaDevAttrMultiProcessorCount, c->device) : cudaErrorInvalidDevice;
+  if (e == cudaSuccess) e = set_attention_attrs();
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  if (e == cudaSuccess) e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found);
+  if (e == cudaSuccess && !fn) e = cudaErrorUnknown;
+  const size_t rows = (size_t)h->sm_count * 2 * (c->max_tokens > A::kTileRows / (c->heads / c->kv_heads) ? 2 * A::kTileRows : A::kTileRows);
+  const size_t o_bytes = rows * c->head_dim * sizeof(float), ml_bytes = rows * sizeof(float2), d_bytes = (size_t)h->sm_count * 8 * sizeof(int);
+  if (e == cudaSuccess) e = cudaMalloc(&h->part_o, o_bytes + ml_bytes + d_bytes + 128);
+  if (e == cudaSuccess) {
+    h->part_ml = reinterpret_cast<float2*>(reinterpret_cast<char*>(h->part_o) + o_bytes);
+    h->desc = reinterpret_cast<int*>(h->part_ml + rows);
+    h->status = h->desc + (size_t)h->sm_count * 8 + 16;
+    // (on a stream of its own: making a handle does not wait for what is queued on the default stream)
+    e = cudaStreamCreateWithFlags(&st, cudaStreamNonBlocking);
+  }
+  if (e == cudaSuccess) e = cudaMemsetAsync(h->status, 0, sizeof(int), st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (st) cudaStreamDestroy(st);
+  if (e != cudaSuccess) {
+    if (g.ok) cudaFree(h->part_o);
+    delete h;
+    return FLY_ERR_CUDA;
+  }
+  h->encode_tiled = reinterpret_cast<PFN_cuTensorMapEncodeTiled>(fn);
   *out = h;
   return FLY_OK;
 }
 
 fly_status_t fly_attention_destroy(fly_attention_t* h) {
+  if (!h) return FLY_OK;
+  DeviceGuard g(h->cfg.device);
+  if (g.ok) cudaFree(h->part_o);
   delete h;
   return FLY_OK;
 }
@@ -148,44 +235,88 @@ fly_status_t fly_attention_run(fly_attention_t* h, const fly_cache_t* c, const f
   if (!h || !a) return FLY_ERR_INVALID_ARG;
   fly_status_t s = check_cache(c, a->B, a->n);
   if (s != FLY_OK || (s = check_rows(&a->q)) != FLY_OK || (s = check_rows(&a->out)) != FLY_OK) return s;
-  if (a->B > h->cfg.max_batch || a->n > h->cfg.max_tokens || c->device != h->cfg.device || c->kv_heads != h->cfg.kv_heads ||
-      c->head_dim != h->cfg.head_dim)
+  const int heads = h->cfg.heads, kv_heads = h->cfg.kv_heads, D = h->cfg.head_dim;
+  if (a->B > h->cfg.max_batch || a->n > h->cfg.max_tokens || c->device != h->cfg.device || c->kv_heads != kv_heads || c->head_dim != D)
     return FLY_ERR_INVALID_ARG;
   if (a->window < 0 || a->sinks < 0 || (a->sinks > 0 && a->window == 0)) return FLY_ERR_INVALID_ARG;
   if (!(a->scale >= 0.0) || !std::isfinite(a->scale)) return FLY_ERR_INVALID_ARG;
-  if (!wide(&a->q, a->B, a->n, h->cfg.heads) || !wide(&a->out, a->B, a->n, h->cfg.heads)) return FLY_ERR_UNSUPPORTED;
-  if ((a->B > 1 && a->q.batch_stride == 0) || (a->n > 1 && a->q.token_stride == 0) || (h->cfg.heads > 1 && a->q.head_stride == 0))
+  if (!wide(&a->q, a->B, a->n, heads) || !wide(&a->out, a->B, a->n, heads)) return FLY_ERR_UNSUPPORTED;
+  if ((a->B > 1 && a->q.batch_stride == 0) || (a->n > 1 && a->q.token_stride == 0) || (heads > 1 && a->q.head_stride == 0))
     return FLY_ERR_UNSUPPORTED;
   DeviceGuard g(h->cfg.device);
   if (!g.ok) return FLY_ERR_CUDA;
-  fly::attn::Params p;
+  A::Params p;
   p.c = view_of(c);
-  p.q = rows_of(&a->q);
   p.out = rows_of(&a->out);
   p.lse = a->lse;
   p.counts = a->counts;
   p.B = a->B;
   p.n = a->n;
-  p.heads = h->cfg.heads;
-  p.group = h->cfg.heads / h->cfg.kv_heads;
-  p.window = a->window;
-  p.sinks = a->sinks;
-  p.scale = (float)((a->scale == 0.0 ? 1.0 / std::sqrt((double)c->head_dim) : a->scale) * 1.4426950408889634);
-  const int64_t blocks = ((int64_t)p.B * p.n * p.heads + 3) / 4;
-  if (blocks > 0x7fffffff) return FLY_ERR_UNSUPPORTED;
-  cudaLaunchConfig_t cfg;
-  cudaLaunchAttribute attr[1];
-  fill_launch(&cfg, attr, (unsigned)blocks, fly::attn::kThreads, static_cast<cudaStream_t>(cuda_stream), true);
+  p.heads = heads;
+  p.group = heads / kv_heads;
+  // (a window that no position is outside of is none)
+  const bool window = a->window > 0 && (int64_t)a->window < (int64_t)p.c.capacity + a->n;
+  p.window = window ? a->window : 0;
+  p.sinks = window ? (a->sinks < p.c.capacity ? a->sinks : p.c.capacity) : 0;
+  p.scale = (float)((a->scale == 0.0 ? 1.0 / std::sqrt((double)D) : a->scale) * 1.4426950408889634);
+  const int most = A::kTileRows / p.group;  // whole tokens in a row tile
+  const bool pair = a->n > most;
+  p.tpt = a->n < most ? a->n : most;
+  p.tpi = pair ? 2 * p.tpt : p.tpt;
+  p.rt = (a->n + p.tpi - 1) / p.tpi;
+  const int64_t groups = (int64_t)p.B * p.rt;
+  if (groups > 1 << 28) return FLY_ERR_UNSUPPORTED;
+  p.groups = (int)groups;
+  p.min_share = 1;
+  p.part_o = h->part_o;
+  p.part_ml = h->part_ml;
+  p.desc = h->desc;
+  p.status = h->status;
   const bool e4m3 = c->format == FLY_CACHE_E4M3;
-  auto kernel = c->head_dim == 128 ? (e4m3 ? fly::attn::attention_kernel<128, true> : fly::attn::attention_kernel<128, false>)
-                                   : (e4m3 ? fly::attn::attention_kernel<64, true> : fly::attn::attention_kernel<64, false>);
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
+  CUtensorMap maps[3];
+  const int64_t qs[3] = {a->q.head_stride, a->q.token_stride, a->q.batch_stride}, ps[3] = {c->token_stride, c->head_stride, c->page_stride};
+  const int64_t qd[4] = {D, heads, p.n, p.B}, pd[4] = {D, c->page_size, kv_heads, c->num_pages};
+  const int qbox[4] = {64, p.group, p.tpt, 1}, pbox[4] = {e4m3 ? D : 64, c->page_size < A::kTile ? c->page_size : A::kTile, 1, 1};
+  if (!encode(h, &maps[0], a->q.data, false, qd, qs, qbox) || !encode(h, &maps[1], c->k_pages, e4m3, pd, ps, pbox) ||
+      !encode(h, &maps[2], c->v_pages, e4m3, pd, ps, pbox))
+    return FLY_ERR_UNSUPPORTED;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  h->last_launches = 0;
+  cudaError_t e = D == 128 ? (e4m3 ? (pair ? launch<128, true, true>(h, maps, p, st) : launch<128, true, false>(h, maps, p, st))
+                                   : (pair ? launch<128, false, true>(h, maps, p, st) : launch<128, false, false>(h, maps, p, st)))
+                           : (e4m3 ? (pair ? launch<64, true, true>(h, maps, p, st) : launch<64, true, false>(h, maps, p, st))
+                                   : (pair ? launch<64, false, true>(h, maps, p, st) : launch<64, false, false>(h, maps, p, st)));
   if (e != cudaSuccess) {
     h->last_cuda_error = (int)e;
     return FLY_ERR_CUDA;
   }
-  h->last_launches = 1;
   return FLY_OK;
+}
+
+fly_status_t fly_attention_device_status(fly_attention_t* h, void* cuda_stream) {
+  if (!h) return FLY_ERR_INVALID_ARG;
+  DeviceGuard g(h->cfg.device);
+  if (!g.ok) return FLY_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  int word = 0;
+  cudaError_t e = cudaMemcpyAsync(&word, h->status, sizeof(int), cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e == cudaSuccess && word != 0) e = cudaMemsetAsync(h->status, 0, sizeof(int), st);
+  if (e != cudaSuccess) {
+    h->last_cuda_error = (int)e;
+    return FLY_ERR_CUDA;
+  }
+  return word == 0 ? FLY_OK : FLY_ERR_TIMEOUT;
+}
+
+fly_status_t fly_attention_selftest_wait(fly_attention_t* h, void* cuda_stream) {
+  if (!h) return FLY_ERR_INVALID_ARG;
+  DeviceGuard g(h->cfg.device);
+  if (!g.ok) return FLY_ERR_CUDA;
+  A::attention_selftest_kernel<<<1, 1, 0, static_cast<cudaStream_t>(cuda_stream)>>>(h->status, 2000000ull);
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) h->last_cuda_error = (int)e;
+  return e == cudaSuccess ? FLY_OK : FLY_ERR_CUDA;
 }
 
 int32_t fly_attention_last_launch_count(const fly_attention_t* h) { return h ? h->last_launches : 0; }

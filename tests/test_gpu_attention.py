@@ -233,6 +233,23 @@ def test_captured_and_replayed_between_plain_calls_and_on_other_streams():
         check_attention(pool, q, out, lse, window=7)
 
 
+def test_a_wait_that_runs_out_is_reported_once_and_shows_in_the_rows():
+    n = 3
+    pool = held([700, 20], n, 1, 64, 16, "bf16", seed=3)
+    att = ChunkAttention(2, n, 8, 1, 64)
+    run(pool, n, 8, handle=att)
+    assert att.device_status(stream()) == Bd.FLY_OK
+    assert att.selftest_wait(stream()) == Bd.FLY_OK
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q = rows(2, n, 8, 64, g)
+    out, lse = torch.zeros_like(q), torch.zeros(2, n, 8, device="cuda")
+    att.run(pool.cache, q, out, lse=lse, stream=stream())            # while the record is pending
+    assert att.device_status(stream()) == Bd.FLY_ERR_TIMEOUT
+    assert bool(out.isnan().all()) and bool(lse.isnan().all())
+    assert att.device_status(stream()) == Bd.FLY_OK
+    run(pool, n, 8, handle=att)
+
+
 def test_refusals():
     pool = held([10, 20], 4, 2, 64)
     g = torch.Generator(device="cuda").manual_seed(8)
