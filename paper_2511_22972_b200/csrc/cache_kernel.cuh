@@ -95,6 +95,41 @@ __device__ __forceinline__ uint2 values_e4m3(uint32_t codes, float scale) {
   return make_uint2(pack_bf16(a * scale, b * scale), pack_bf16(c * scale, d * scale));
 }
 
+// Sixteen codes as eight pairs of bf16, scaled, for where conversions are what there is to do.  Placed into a bf16's bits (sign, then exponent and
+// mantissa four places lower) a code reads as its value times 2^-120, subnormal codes as subnormal bf16; one multiplication by
+// 2^(s - 7) puts both right.  Not so for scales above 134 and for code 0x7f (NaN, which append never writes): plain4_e4m3 says whether
+// 4 x 16 codes are without, and any16_e4m3 takes all.
+__device__ __forceinline__ bool plain4_e4m3(const uint4 (&c)[4], const int (&s)[4]) {
+  uint32_t nan = 0u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    nan |= ((c[i].x & 0x7f7f7f7fu) + 0x01010101u) | ((c[i].y & 0x7f7f7f7fu) + 0x01010101u) | ((c[i].z & 0x7f7f7f7fu) + 0x01010101u) |
+           ((c[i].w & 0x7f7f7f7fu) + 0x01010101u);
+  return (nan & 0x80808080u) == 0u && max(max(s[0], s[1]), max(s[2], s[3])) <= 134;
+}
+__device__ __forceinline__ void plain16_e4m3(const uint4& codes, int s, uint32_t (&w)[8]) {
+  const uint32_t c[4] = {codes.x, codes.y, codes.z, codes.w}, f = (uint32_t)(s + 120) * 0x00800080u;  // 2^(s - 7) twice
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint32_t h = __byte_perm(c[i], 0u, k ? 0x3424 : 0x1404);  // two codes in the upper bytes
+      const uint32_t v = (h & 0x80008000u) | ((h >> 4) & 0x07f007f0u);
+      asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(w[2 * i + k]) : "r"(v), "r"(f));
+    }
+  }
+}
+__device__ __forceinline__ void any16_e4m3(const uint4& codes, int s, uint32_t (&w)[8]) {
+  const uint32_t c[4] = {codes.x, codes.y, codes.z, codes.w};
+  const float scale = scale_value(s);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint2 v = values_e4m3(c[i], scale);
+    w[2 * i] = v.x;
+    w[2 * i + 1] = v.y;
+  }
+}
+
 // Eight consecutive bf16.  wide: the address is a whole number of 16 bytes.
 __device__ __forceinline__ uint4 load8(const uint8_t* p, bool wide) {
   if (wide) return *reinterpret_cast<const uint4*>(p);

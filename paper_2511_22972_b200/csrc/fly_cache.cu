@@ -15,7 +15,7 @@
 struct fly_attention {
   fly_attention_config_t cfg;
   int sm_count = 148;
-  float* part_o = nullptr;  // one block: parts of items | their references and sums | how the ranges begin | status word
+  float4* part_o = nullptr;  // one block: parts of items | their references and sums | how the ranges begin | status word
   float2* part_ml = nullptr;
   int* desc = nullptr;
   int* status = nullptr;
@@ -109,19 +109,36 @@ cudaError_t set_attention_attrs() {
   return e;
 }
 
-// A four-dimensional tensor of bf16 (128-byte swizzle) or of codes (as they lie); dims[0] contiguous, strides in elements.
-bool encode(fly_attention* h, CUtensorMap* map, const void* data, bool codes, const int64_t* dims, const int64_t* strides, const int* box) {
-  const int esz = codes ? 1 : 2;
-  cuuint64_t d[4], s[3];
-  cuuint32_t b[4], one[4] = {1, 1, 1, 1};
-  for (int i = 0; i < 4; ++i) {
-    d[i] = (cuuint64_t)dims[i];
-    b[i] = (cuuint32_t)box[i];
+// The queries [B, n, heads, D] in boxes of 64 values x the heads of a group x the tokens of a row tile.
+bool encode_q(fly_attention* h, CUtensorMap* map, const fly_rows_t* q, const A::Params& p) {
+  const cuuint64_t D = (cuuint64_t)h->cfg.head_dim;
+  const cuuint64_t dims[4] = {D, (cuuint64_t)p.heads, (cuuint64_t)p.n, (cuuint64_t)p.B};
+  const int64_t strides[3] = {q->head_stride, q->token_stride, q->batch_stride};
+  cuuint64_t bytes[3];
+  for (int i = 0; i < 3; ++i) bytes[i] = 2 * (dims[i + 1] > 1 ? (cuuint64_t)strides[i] : D);  // (of a dimension of one entry: anything)
+  const cuuint32_t box[4] = {64, (cuuint32_t)p.group, (cuuint32_t)p.tpt, 1}, one[4] = {1, 1, 1, 1};
+  return h->encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, q->data, dims, bytes, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Pages.  bf16: boxes of eight tokens with all their values, 64 at a time and swizzled.  E4M3: boxes of a page's (or 128) tokens' codes as they lie.
+bool encode_pages(fly_attention* h, CUtensorMap* map, const fly_cache_t* c, void* pages) {
+  const bool e4m3 = c->format == FLY_CACHE_E4M3;
+  const cuuint64_t D = (cuuint64_t)c->head_dim, esz = e4m3 ? 1 : 2;
+  const cuuint64_t token = (cuuint64_t)c->token_stride * esz;
+  const cuuint64_t head = c->kv_heads > 1 ? (cuuint64_t)c->head_stride * esz : D * esz, page = c->num_pages > 1 ? (cuuint64_t)c->page_stride * esz : D * esz;
+  const cuuint64_t tokens = (cuuint64_t)c->page_size, heads = (cuuint64_t)c->kv_heads, count = (cuuint64_t)c->num_pages;
+  const cuuint32_t one[5] = {1, 1, 1, 1, 1};
+  if (e4m3) {
+    const cuuint64_t dims[4] = {D, tokens, heads, count}, bytes[3] = {token, head, page};
+    const cuuint32_t box[4] = {(cuuint32_t)D, (cuuint32_t)(c->page_size < A::kTile ? c->page_size : A::kTile), 1, 1};
+    return h->encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, pages, dims, bytes, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                           CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
   }
-  for (int i = 0; i < 3; ++i) s[i] = (cuuint64_t)(dims[i + 1] > 1 ? strides[i] : dims[0]) * esz;  // (of a dimension of one entry: anything)
-  return h->encode_tiled(map, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(data), d, s, b, one,
-                         CU_TENSOR_MAP_INTERLEAVE_NONE, codes ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
-                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const cuuint64_t dims[5] = {64, tokens, D / 64, heads, count}, bytes[4] = {token, 128, head, page};
+  const cuuint32_t box[5] = {64, 8, (cuuint32_t)(D / 64), 1, 1};
+  return h->encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, pages, dims, bytes, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int D, bool E4M3, bool PAIR>
@@ -134,10 +151,10 @@ cudaError_t launch(fly_attention* h, const CUtensorMap* maps, const A::Params& p
   cudaError_t e = cudaLaunchKernelEx(&cfg, A::attention_kernel<D, E4M3, PAIR>, maps[0], maps[1], maps[2], p);
   if (e != cudaSuccess || h->sm_count < 2) return e;
   h->last_launches++;
-  fill_launch(&cfg, attr, (unsigned)h->sm_count - 1, A::kCombineThreads, st, true);
+  fill_launch(&cfg, attr, (unsigned)h->sm_count - 1, D * 8, st, true);
   const int used = PAIR ? S::kItemRows : p.tpt * p.group;
-  cfg.gridDim.y = (unsigned)((used + A::kCombineThreads / 32 - 1) / (A::kCombineThreads / 32));
-  e = cudaLaunchKernelEx(&cfg, A::attention_combine_kernel<D>, p, (int)S::kItemRows);
+  cfg.gridDim.y = (unsigned)((used + 31) / 32);
+  e = cudaLaunchKernelEx(&cfg, A::attention_combine_kernel<D, S::kItemRows>, p);
   if (e == cudaSuccess) h->last_launches++;
   return e;
 }
@@ -265,7 +282,8 @@ fly_status_t fly_attention_run(fly_attention_t* h, const fly_cache_t* c, const f
   p.tpi = pair ? 2 * p.tpt : p.tpt;
   p.rt = (a->n + p.tpi - 1) / p.tpi;
   const int64_t groups = (int64_t)p.B * p.rt;
-  if (groups > 1 << 28) return FLY_ERR_UNSUPPORTED;
+  // (tiles of positions are counted in 32 bits, lengths are not known here)
+  if (groups > 1 << 28 || groups * kv_heads * ((int64_t)p.c.capacity / A::kTile + 2) > 0x7fffffff) return FLY_ERR_UNSUPPORTED;
   p.groups = (int)groups;
   p.min_share = 1;
   p.part_o = h->part_o;
@@ -274,11 +292,7 @@ fly_status_t fly_attention_run(fly_attention_t* h, const fly_cache_t* c, const f
   p.status = h->status;
   const bool e4m3 = c->format == FLY_CACHE_E4M3;
   CUtensorMap maps[3];
-  const int64_t qs[3] = {a->q.head_stride, a->q.token_stride, a->q.batch_stride}, ps[3] = {c->token_stride, c->head_stride, c->page_stride};
-  const int64_t qd[4] = {D, heads, p.n, p.B}, pd[4] = {D, c->page_size, kv_heads, c->num_pages};
-  const int qbox[4] = {64, p.group, p.tpt, 1}, pbox[4] = {e4m3 ? D : 64, c->page_size < A::kTile ? c->page_size : A::kTile, 1, 1};
-  if (!encode(h, &maps[0], a->q.data, false, qd, qs, qbox) || !encode(h, &maps[1], c->k_pages, e4m3, pd, ps, pbox) ||
-      !encode(h, &maps[2], c->v_pages, e4m3, pd, ps, pbox))
+  if (!encode_q(h, &maps[0], &a->q, p) || !encode_pages(h, &maps[1], c, c->k_pages) || !encode_pages(h, &maps[2], c, c->v_pages))
     return FLY_ERR_UNSUPPORTED;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   h->last_launches = 0;
