@@ -157,16 +157,24 @@ __device__ __forceinline__ void tmem_ld32(uint32_t a, uint32_t (&r)[32]) {
   tmem_ask32(a, r);
   tmem_wait(r);
 }
-__device__ __forceinline__ void tmem_st16(uint32_t a, const uint32_t (&r)[16]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(a), FLY_I8(r, 0),
-               FLY_I8(r, 8)
+// The same for 16 columns, and a wait for two of them.
+__device__ __forceinline__ void tmem_ask16(uint32_t a, uint32_t (&r)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+               : FLY_R8(r, 0), FLY_R8(r, 8)
+               : "r"(a)
                : "memory");
+}
+__device__ __forceinline__ void tmem_wait16(uint32_t (&r)[16], uint32_t (&q)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : FLY_W8(r, 0), FLY_W8(r, 8), FLY_W8(q, 0), FLY_W8(q, 8) : : "memory");
 }
 __device__ __forceinline__ void tmem_st32(uint32_t a, const uint32_t (&r)[32]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,"
       "%26,%27,%28,%29,%30,%31,%32};" ::"r"(a), FLY_I8(r, 0), FLY_I8(r, 8), FLY_I8(r, 16), FLY_I8(r, 24)
       : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t a, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(a), FLY_I8(r, 0) : "memory");
 }
 #undef FLY_R8
 #undef FLY_W8
@@ -230,8 +238,18 @@ __device__ __forceinline__ Range range_of(const Params& p) {  // (the host has s
   int sum = count0;
 #pragma unroll 4
   for (int g = 32 + lane; g < p.groups; g += 32) sum += group_at(p, g).count * p.c.kv_heads;
+  int x0 = count0;  // over the first 32 groups
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  for (int d = 1; d < 32; d <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x0, d);
+    if (lane >= d) x0 += y;
+  }
+  if (p.groups > 32) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  } else {
+    sum = __shfl_sync(0xffffffffu, x0, 31);
+  }
   r.share = max(p.min_share, (int)(((uint32_t)sum + gridDim.x - 1u) / gridDim.x));
   const uint32_t begin = (uint32_t)r.share * blockIdx.x;  // (at most sum + grid)
   r.g = r.off = r.tiles = 0;
@@ -242,11 +260,14 @@ __device__ __forceinline__ Range range_of(const Params& p) {  // (the host has s
   for (int base = 0;; base += 32) {
     if (base > 0) g0 = group_at(p, min(base + lane, p.groups - 1));
     const int v = base == 0 ? count0 : base + lane < p.groups ? g0.count * p.c.kv_heads : 0;
-    int x = v;
+    int x = x0;
+    if (base > 0) {
+      x = v;
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, x, d);
-      if (lane >= d) x += y;
+      for (int d = 1; d < 32; d <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, d);
+        if (lane >= d) x += y;
+      }
     }
     const unsigned past = __ballot_sync(0xffffffffu, run + x > first);
     if (past) {  // (first < sum: some lane is past it)
@@ -332,6 +353,20 @@ __device__ __forceinline__ bool tile_partial(const Params& p, const Group& g, in
   return (p0 + kTile > g.L + g.t0 + 1 && g.hi > max(p0, g.L + g.t0 + 1)) ||
          (p0 < g.lo_last && p0 + kTile > max(p.sinks, g.lo_first) && g.lo_first < g.lo_last);
 }
+// The part of a tile that the second MMA has to take, relative to the tile: positions first .. last - 1, without hole0 .. hole1 - 1 (between the
+// first tokens and the window) and what stands on missing pages.
+struct Span {
+  int first, last, hole0, hole1;
+};
+__device__ __forceinline__ Span tile_span(const Params& p, const Group& g, int p0) {
+  Span s;
+  const int lo = g.lo_first - p0, end = min(g.hi - p0, kTile), early = p.sinks - p0;
+  s.first = early > 0 ? 0 : max(lo, 0);
+  s.last = early > 0 && lo >= end ? min(early, end) : end;
+  s.hole0 = max(early, 0);
+  s.hole1 = early > 0 ? min(lo, s.last) : 0;
+  return s;
+}
 __device__ __forceinline__ uint32_t zero_nonfinite(uint32_t w, bool& any) {  // a pair of bf16
   if ((w & 0x7f80u) == 0x7f80u) { w &= 0xffff0000u; any = true; }
   if ((w & 0x7f800000u) == 0x7f800000u) { w &= 0xffffu; any = true; }
@@ -360,13 +395,19 @@ struct RowMask {
     return v;
   }
 };
-template <bool MASK>
-__device__ __forceinline__ void hide(uint32_t (&r)[32], const RowMask& mask, int c0) {
-  if (!MASK) return;
-  const uint32_t v = mask.bits(c0);
+// Scores that a row does not see become -inf, in tensor memory, for tiles where there are any.  32 columns at a time in a loop: code that runs
+// once an item is fetched anew each time, about four cycles an instruction, and as part of the unrolled step below the mask took 4000 cycles.
+__device__ __forceinline__ void hide(uint32_t ts, const RowMask& mask) {
+  uint32_t r[32];
+#pragma unroll 1
+  for (int c0 = 0; c0 < kTile; c0 += 32) {
+    tmem_ld32(ts + c0, r);
+    const uint32_t v = mask.bits(c0);
 #pragma unroll
-  for (int c = 0; c < 32; ++c)
-    if (!((v >> c) & 1u)) r[c] = 0xff800000u;
+    for (int c = 0; c < 32; ++c) r[c] = v & (1u << c) ? r[c] : 0xff800000u;
+    tmem_st32(ts + c0, r);
+  }
+  tmem_st_wait();
 }
 __device__ __forceinline__ float max32(const uint32_t (&r)[32], float mx) {
   float m[4];
@@ -376,15 +417,21 @@ __device__ __forceinline__ float max32(const uint32_t (&r)[32], float mx) {
   for (int c = 4; c < 32; ++c) m[c & 3] = fmaxf(m[c & 3], __uint_as_float(r[c]));
   return fmaxf(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), mx);
 }
-__device__ __forceinline__ void exp32(const uint32_t (&r)[32], f2 sc2, f2 nr2, f2 (&acc)[2], uint32_t (&w)[16]) {
+// 32 exponentials; their bf16 go to tensor memory at `to`.
+__device__ __forceinline__ void exp32(const uint32_t (&r)[32], f2 sc2, f2 nr2, f2 (&acc)[2], uint32_t to) {
 #pragma unroll
-  for (int c = 0; c < 32; c += 2) {
-    float x, y;
-    unpack2(fma2(pack2(__uint_as_float(r[c]), __uint_as_float(r[c + 1])), sc2, nr2), x, y);
-    x = ex2_approx(x);
-    y = ex2_approx(y);
-    acc[(c >> 1) & 1] = add2(acc[(c >> 1) & 1], pack2(x, y));
-    w[c / 2] = cache::pack_bf16(x, y);
+  for (int h = 0; h < 32; h += 16) {
+    uint32_t w[8];
+#pragma unroll
+    for (int c = 0; c < 16; c += 2) {
+      float x, y;
+      unpack2(fma2(pack2(__uint_as_float(r[h + c]), __uint_as_float(r[h + c + 1])), sc2, nr2), x, y);
+      x = ex2_approx(x);
+      y = ex2_approx(y);
+      acc[(c >> 1) & 1] = add2(acc[(c >> 1) & 1], pack2(x, y));
+      w[c / 2] = cache::pack_bf16(x, y);
+    }
+    tmem_st8(to + h / 2, w);
   }
 }
 
@@ -393,23 +440,19 @@ constexpr int kOffP = 64;  // P's first column over S: its columns are taken fro
 // One step of a row: S in tensor memory at `ts` becomes P there, the row's reference and sum move on, and O at `to` is rescaled if it must be.
 // Columns come 32 at a time, the next ones on their way while one block is worked on; the last block of the maximum is the
 // first of the exponentials.
-template <int D, bool MASK>
-__device__ __forceinline__ void softmax_step(uint32_t ts, uint32_t to, float scale, bool first, const RowMask& mask, float& ref, float& sum) {
-  uint32_t a[32], b[32], w[16];
+template <int D>
+__device__ __forceinline__ void softmax_step(uint32_t ts, uint32_t to, float scale, bool first, float& ref, float& sum) {
+  uint32_t a[32], b[32];
   tmem_ld32(ts, a);
   tmem_ask32(ts + 32, b);
-  hide<MASK>(a, mask, 0);
   float mx = max32(a, -INFINITY);
   tmem_wait(b);
   tmem_ask32(ts + 64, a);
-  hide<MASK>(b, mask, 32);
   mx = max32(b, mx);
   tmem_wait(a);
   tmem_ask32(ts + 96, b);
-  hide<MASK>(a, mask, 64);
   mx = max32(a, mx);
   tmem_wait(b);
-  hide<MASK>(b, mask, 96);
   mx = max32(b, mx);
   const float top = mx * scale;
   const bool move = top > ref + 8.0f;  // (false for a row that has seen nothing, and for NaN)
@@ -430,29 +473,21 @@ __device__ __forceinline__ void softmax_step(uint32_t ts, uint32_t to, float sca
   const float nr = ref == -INFINITY ? 0.f : -ref;
   const f2 sc2 = pack2(scale, scale), nr2 = pack2(nr, nr);
   f2 acc[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
-  tmem_ask32(ts + 64, a);
-  exp32(b, sc2, nr2, acc, w);
-  tmem_st16(ts + kOffP + 48, w);
-  tmem_wait(a);
-  tmem_ask32(ts + 32, b);
-  hide<MASK>(a, mask, 64);
-  exp32(a, sc2, nr2, acc, w);
-  tmem_st16(ts + kOffP + 32, w);
-  tmem_wait(b);
-  tmem_ask32(ts, a);
-  hide<MASK>(b, mask, 32);
-  exp32(b, sc2, nr2, acc, w);
-  tmem_st16(ts + kOffP + 16, w);
-  tmem_wait(a);
-  hide<MASK>(a, mask, 0);
-  exp32(a, sc2, nr2, acc, w);
-  tmem_st16(ts + kOffP, w);
+#pragma unroll 1
+  for (int h = 1; h >= 0; --h) {
+    tmem_ask32(ts + h * 64, a);
+    exp32(b, sc2, nr2, acc, ts + kOffP + h * 32 + 16);
+    tmem_wait(a);
+    if (h != 0) tmem_ask32(ts + 32, b);
+    exp32(a, sc2, nr2, acc, ts + kOffP + h * 32);
+    if (h != 0) tmem_wait(b);
+  }
   float x, y;
   unpack2(add2(acc[0], acc[1]), x, y);
   sum += x + y;
 }
 
-// Adds back to a row what zero_nonfinite took out of the values that it sees; columns col0 .. col0 + 31 of row_pos are in o.
+// Adds back to a row what zero_nonfinite took out of the values that it sees; columns col0 .. col0 + 15 of row_pos are in o.
 template <bool E4M3>
 __device__ __noinline__ void add_back(const Params& p, int b, int kvh, int row_pos, int lo_first, int lo_last, int upper, int hi, int col0, float* o) {
   auto visit = [&](int from, int to) {
@@ -463,7 +498,7 @@ __device__ __noinline__ void add_back(const Params& p, int b, int kvh, int row_p
       const int slot = pos & ((1 << p.c.page_shift) - 1);
       const int64_t at = cache::row_at(p.c, page, slot, kvh) + col0;
       const float scale = E4M3 ? cache::scale_value(p.c.v_scales[cache::scale_at(p.c, page, slot, kvh)]) : 1.f;
-      for (int c = 0; c < 32; c += 2) {
+      for (int c = 0; c < 16; c += 2) {
         float x, y;
         if (E4M3) {
           cache::unpack_e4m3(*reinterpret_cast<const uint16_t*>(p.c.v_pages + at + c), x, y);
@@ -557,6 +592,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
   uint32_t ring = 0;     // tiles of keys and values that went through the ring before this item
   uint32_t tile_no = 0;  // tiles of positions before this item
 
+  if (warp >= 8 && warp < S::kWarpConv) {
   if (warp == S::kWarpK || warp == S::kWarpV) {
     // ---------------- keys, or values: a lane per box ----------------
     const bool values = warp == S::kWarpV;
@@ -566,7 +602,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     const uint32_t box_bytes = (uint32_t)rows * D * (E4M3 ? 1 : 2);
     constexpr int kRing = E4M3 ? S::kRawStages : S::kStages;
     for (; walk.have(); walk.next()) {
-      const Group g = walk.gr;
+      const Group& g = walk.gr;
       const int m = walk.tiles();
       int page = tile_page(p, g, walk.x0);
       for (int j = 0; j < m; ++j) {
@@ -609,77 +645,6 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       ring += 2u * m;
       tile_no += m;
     }
-  } else if (E4M3 && warp >= S::kWarpConv) {
-    // ---------------- codes to tiles of bf16, 16 at a time ----------------
-    // Eight neighbouring threads take four chunks of two rows, whose places in the swizzled tile share no bank.  From one of its chunks to the
-    // next a thread goes on by whole groups of eight rows: its place in a row and in the swizzle stays.
-    constexpr int kPer = D / 64, kConv = E4M3 ? S::kConvThreads : 128, kEach = kTile * D / 16 / kConv, kRowStep = kConv / 8 / kPer * 2;
-    const int ct = tid - S::kWarpConv * 32;
-    const int row0 = (ct >> 3) / kPer * 2 + ((ct >> 2) & 1), chunk = (ct >> 3) % kPer * 4 + (ct & 3);
-    const int from0 = row0 * D + chunk * 16, to0 = S::piece_at(row0, chunk * 2), to1 = S::piece_at(row0, chunk * 2 + 1);
-    constexpr int kToStep = kRowStep / 8 * S::kGroupBytes;
-    uint32_t item = 0;
-    for (; walk.have(); walk.next(), ++item) {
-      const Group g = walk.gr;
-      const int m = walk.tiles();
-      auto convert = [&](int place, bool values, int j) {
-        const uint32_t idx = ring + (uint32_t)place;
-        constexpr uint32_t kRing = S::kRawStages > 0 ? S::kRawStages : 1;
-        const int rs = (int)(idx % kRing), st = (int)(idx % S::kStages);
-        wait_warp(raw_full(rs), (idx / kRing) & 1);
-        wait_warp(empty(st), ((idx / S::kStages) & 1) ^ 1);
-        const uint8_t* raw = smem + S::kOffRaw + rs * S::kRawBytes;
-        uint8_t* dst = smem + S::kOffRing + st * S::kTileBytes;
-        const int p0 = tile_start(g, walk.x0 + j);
-        const uint32_t bad = tile_bad[(tile_no + (uint32_t)j) & 15];
-        const bool edge = values && (bad != 0 || tile_unseen(p, g, p0) || tile_partial(p, g, p0));
-        bool any = false;
-#pragma unroll
-        for (int i0 = 0; i0 < kEach; i0 += 4) {
-          uint4 codes[4];
-          int scale[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            codes[i] = *reinterpret_cast<const uint4*>(raw + from0 + (i0 + i) * kRowStep * D);
-            scale[i] = raw[S::kRawTile + row0 + (i0 + i) * kRowStep];
-          }
-          uint32_t w[4][8];
-          if (!cache::plain4_e4m3(codes, scale)) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) cache::any16_e4m3(codes[i], scale[i], w[i]);
-          } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) cache::plain16_e4m3(codes[i], scale[i], w[i]);
-          }
-          if (edge) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int row = row0 + (i0 + i) * kRowStep, seen = (bad >> (row >> 3)) & 1u ? 0 : seen_by(p, g, p0 + row);
-#pragma unroll
-              for (int k = 0; k < 8; ++k) w[i][k] = seen == 0 ? 0u : seen == 1 ? zero_nonfinite(w[i][k], any) : w[i][k];
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            *reinterpret_cast<uint4*>(dst + to0 + (i0 + i) * kToStep) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
-            *reinterpret_cast<uint4*>(dst + to1 + (i0 + i) * kToStep) = make_uint4(w[i][4], w[i][5], w[i][6], w[i][7]);
-          }
-        }
-        if (any) misc[8 + (item & 7)] = item + 1;
-        async_proxy_fence();
-        if (!failed) {
-          mbar_arrive(full(st));
-          mbar_arrive(raw_empty(rs));
-        }
-        __syncwarp();
-      };
-      for (int j = 0; j <= m; ++j) {  // K(0) [V(0)] K(1) V(0 or 1) ...
-        if (j < m) convert(ring_k<PAIR>(j), false, j);
-        if (PAIR ? j < m : j > 0) convert(ring_v<PAIR>(PAIR ? j : j - 1, m), true, PAIR ? j : j - 1);
-      }
-      ring += 2u * m;
-      tile_no += m;
-    }
   } else if (warp == S::kWarpQ) {
     // ---------------- queries: (heads of the group, tokens) boxes; tokens behind the chunk's end come as zeros ----------------
     uint32_t item = 0;
@@ -719,7 +684,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     constexpr uint32_t kIdescS = instr_desc(kTile, false), kIdescO = instr_desc(D, true);
     uint32_t item = 0, use0 = 0, use1 = 0;  // steps of each slot so far
     for (; walk.have(); walk.next(), ++item) {
-      const Group g = walk.gr;
+      const Group& g = walk.gr;
       const int m = walk.tiles();
       auto sees = [&](int s, int j) { return !PAIR || slot_sees(p, g, s, tile_start(g, walk.x0 + j)); };
       auto issue_s = [&](int s, int j) {  // S of slot s = Q x keys of tile j
@@ -735,7 +700,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         }
         __syncwarp();
       };
-      auto issue_o = [&](int s, int j, bool accumulate) {  // O of slot s += P x values of tile j
+      auto issue_o = [&](int s, int j, bool accumulate) {  // O of slot s += P x values of tile j, 16 positions at a time
         uint32_t& use = s ? use1 : use0;
         wait_warp(p_ready(s), use & 1);
         ++use;
@@ -743,10 +708,18 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         tc_fence_after();
         if (!failed && lead) {
           const uint32_t b = desc_lo(base + S::kOffRing + st * S::kTileBytes, 1024);
+          const uint32_t to = tmem + 2 * kTile + s * 128, from = tmem + s * kTile + kOffP;
+          const Span span = tile_span(p, g, tile_start(g, walk.x0 + j));
+          if (span.first == 0 && span.last == kTile) {
 #pragma unroll
-          for (int k = 0; k < kTile / 16; ++k)
-            mma_ts(tmem + 2 * kTile + s * 128, tmem + s * kTile + kOffP + k * 8, b + ((uint32_t)(k * 2 * S::kGroupBytes) >> 4), desc_hi(S::kGroupBytes), kIdescO,
-                   accumulate || k != 0);
+            for (int k = 0; k < kTile / 16; ++k)
+              mma_ts(to, from + k * 8, b + ((uint32_t)(k * 2 * S::kGroupBytes) >> 4), desc_hi(S::kGroupBytes), kIdescO, accumulate || k != 0);
+          } else {
+            const int k0 = span.first / 16;
+#pragma unroll 1
+            for (int k = k0; k * 16 < span.last; ++k)
+              mma_ts(to, from + k * 8, b + ((uint32_t)(k * 2 * S::kGroupBytes) >> 4), desc_hi(S::kGroupBytes), kIdescO, accumulate || k != k0);
+          }
         }
         __syncwarp();
       };
@@ -816,6 +789,78 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       while (global_ns() - t0 < 2000000ull) {}
     }
     __syncwarp();
+  }
+  } else if (E4M3 && warp >= S::kWarpConv) {
+    // ---------------- codes to tiles of bf16, 16 at a time ----------------
+    // Eight neighbouring threads take four chunks of two rows, whose places in the swizzled tile share no bank.  From one of its chunks to the
+    // next a thread goes on by whole groups of eight rows: its place in a row and in the swizzle stays.
+    constexpr int kPer = D / 64, kConv = E4M3 ? S::kConvThreads : 128, kEach = kTile * D / 16 / kConv, kRowStep = kConv / 8 / kPer * 2;
+    const int ct = tid - S::kWarpConv * 32;
+    const int row0 = (ct >> 3) / kPer * 2 + ((ct >> 2) & 1), chunk = (ct >> 3) % kPer * 4 + (ct & 3);
+    const int from0 = row0 * D + chunk * 16, to0 = S::piece_at(row0, chunk * 2), to1 = S::piece_at(row0, chunk * 2 + 1);
+    constexpr int kToStep = kRowStep / 8 * S::kGroupBytes;
+    uint32_t item = 0;
+    for (; walk.have(); walk.next(), ++item) {
+      const Group& g = walk.gr;
+      const int m = walk.tiles();
+      auto convert = [&](int place, bool values, int j) {
+        const uint32_t idx = ring + (uint32_t)place;
+        constexpr uint32_t kRing = S::kRawStages > 0 ? S::kRawStages : 1;
+        const int rs = (int)(idx % kRing), st = (int)(idx % S::kStages);
+        wait_warp(raw_full(rs), (idx / kRing) & 1);
+        wait_warp(empty(st), ((idx / S::kStages) & 1) ^ 1);
+        const uint8_t* raw = smem + S::kOffRaw + rs * S::kRawBytes;
+        uint8_t* dst = smem + S::kOffRing + st * S::kTileBytes;
+        const int p0 = tile_start(g, walk.x0 + j);
+        const uint32_t bad = tile_bad[(tile_no + (uint32_t)j) & 15];
+        const bool edge = values && (bad != 0 || tile_unseen(p, g, p0) || tile_partial(p, g, p0));
+        bool any = false;
+#pragma unroll
+        for (int i0 = 0; i0 < kEach; i0 += 4) {
+          uint4 codes[4];
+          int scale[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            codes[i] = *reinterpret_cast<const uint4*>(raw + from0 + (i0 + i) * kRowStep * D);
+            scale[i] = raw[S::kRawTile + row0 + (i0 + i) * kRowStep];
+          }
+          uint32_t w[4][8];
+          if (!cache::plain4_e4m3(codes, scale)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) cache::any16_e4m3(codes[i], scale[i], w[i]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) cache::plain16_e4m3(codes[i], scale[i], w[i]);
+          }
+          if (edge) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int row = row0 + (i0 + i) * kRowStep, seen = (bad >> (row >> 3)) & 1u ? 0 : seen_by(p, g, p0 + row);
+#pragma unroll
+              for (int k = 0; k < 8; ++k) w[i][k] = seen == 0 ? 0u : seen == 1 ? zero_nonfinite(w[i][k], any) : w[i][k];
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            *reinterpret_cast<uint4*>(dst + to0 + (i0 + i) * kToStep) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
+            *reinterpret_cast<uint4*>(dst + to1 + (i0 + i) * kToStep) = make_uint4(w[i][4], w[i][5], w[i][6], w[i][7]);
+          }
+        }
+        if (any) misc[8 + (item & 7)] = item + 1;
+        async_proxy_fence();
+        if (!failed) {
+          mbar_arrive(full(st));
+          mbar_arrive(raw_empty(rs));
+        }
+        __syncwarp();
+      };
+      for (int j = 0; j <= m; ++j) {  // K(0) [V(0)] K(1) V(0 or 1) ...
+        if (j < m) convert(ring_k<PAIR>(j), false, j);
+        if (PAIR ? j < m : j > 0) convert(ring_v<PAIR>(PAIR ? j : j - 1, m), true, PAIR ? j : j - 1);
+      }
+      ring += 2u * m;
+      tile_no += m;
+    }
   } else {
     // ---------------- softmax of a slot, a thread per row ----------------
     const int slot = warp >> 2, row = tid & 127, quarter = warp & 3;
@@ -824,7 +869,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     const int row_token = row / p.group, row_head = row - row_token * p.group;
     uint32_t use = 0, items_done = 0, item = 0;
     for (; walk.have(); walk.next(), ++item) {
-      const Group g = walk.gr;
+      const Group& g = walk.gr;
       const int m = walk.tiles();
       const int ts0 = g.t0 + (PAIR ? slot * p.tpt : 0), ts1 = min(g.t1, ts0 + p.tpt);  // the slot's tokens
       const int t = ts0 + row_token, row_pos = g.L + t;
@@ -841,45 +886,50 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         const uint32_t bad = tile_bad[(tile_no + (uint32_t)j) & 15];
         if (warp_live) {
           tc_fence_after();
-          RowMask mask;
-          mask.bad = bad;
-          if (p0 + kTile > first_hi || (p0 < last_lo && p0 + kTile > p.sinks) || mask.bad != 0) {
+          if (p0 + kTile > first_hi || (p0 < last_lo && p0 + kTile > p.sinks) || bad != 0) {
+            RowMask mask;
+            mask.bad = bad;
             mask.lim = min(row_pos + 1, g.hi) - p0;
             mask.lo = p.window > 0 ? row_pos + 1 - p.window - p0 : 0;
             mask.snk = p.sinks - p0;
-            softmax_step<D, true>(ts, to, p.scale, !begun, mask, ref, sum);
-          } else {
-            softmax_step<D, false>(ts, to, p.scale, !begun, mask, ref, sum);
+            hide(ts, mask);
           }
+          softmax_step<D>(ts, to, p.scale, !begun, ref, sum);
           tmem_st_wait();
           tc_fence_before();
         }
         if (!E4M3 && (bad != 0 || tile_unseen(p, g, p0) || tile_partial(p, g, p0)) && (!PAIR || slot == 0 || !slot_sees(p, g, 0, p0))) {
-          // The values' tile before its MMAs (those of both slots come after this slot's p_ready): 16 bytes at a time.
+          // The values' tile before its MMAs (those of both slots come after this slot's p_ready), 16 bytes at a time: only what the MMAs take.
           const uint32_t idx = ring + (uint32_t)ring_v<PAIR>(j, m);
           const int st = (int)(idx % S::kStages);
           wait(full(st), (idx / S::kStages) & 1);
           uint8_t* tile = smem + S::kOffRing + st * S::kTileBytes;
+          const Span span = tile_span(p, g, p0);
           bool any = false;
-#pragma unroll 4
-          for (int i = 0; i < D / 8; ++i) {  // a row of the tile: one or two warps' neighbours
-            const int r = i * (kTileRows / (D / 8)) + row / (D / 8), piece = row % (D / 8);
-            const int seen = (bad >> (r >> 3)) & 1u ? 0 : seen_by(p, g, p0 + r);
-            uint4* at = reinterpret_cast<uint4*>(tile + S::piece_at(r, piece));
-            if (seen == 0) *at = make_uint4(0u, 0u, 0u, 0u);
-            if (seen == 1) {
-              uint4 v = *at;
-              bool here = false;
-              v.x = zero_nonfinite(v.x, here);
-              v.y = zero_nonfinite(v.y, here);
-              v.z = zero_nonfinite(v.z, here);
-              v.w = zero_nonfinite(v.w, here);
-              if (here) {
-                *at = v;
-                any = true;
+          auto clean = [&](int from, int to_row, bool zero) {  // rows from .. to_row - 1
+#pragma unroll 1
+            for (int u = row; u < (to_row - from) * (D / 8); u += kTileRows) {
+              uint4* at = reinterpret_cast<uint4*>(tile + S::piece_at(from + u / (D / 8), u % (D / 8)));
+              uint4 v = zero ? make_uint4(0u, 0u, 0u, 0u) : *at;
+              bool here = zero;
+              if (!zero) {
+                v.x = zero_nonfinite(v.x, here);
+                v.y = zero_nonfinite(v.y, here);
+                v.z = zero_nonfinite(v.z, here);
+                v.w = zero_nonfinite(v.w, here);
+                any |= here;
               }
+              if (here) *at = v;
             }
-          }
+          };
+          const int upper = g.L + g.t0 + 1 - p0, window0 = max(max(g.lo_first, p.sinks) - p0, 0), window1 = min(g.lo_last - p0, min(upper, span.last));
+#pragma unroll 1
+          for (int i = 0; i < 5; ++i)  // nobody sees them | later rows only, earlier rows only
+            clean(i == 0 ? span.first & ~15 : i == 1 ? span.last : i == 2 ? span.hole0 : i == 3 ? max(upper, 0) : window0,
+                  i == 0 ? span.first : i == 1 ? (span.last + 15) & ~15 : i == 2 ? span.hole1 : i == 3 ? span.last : window1, i < 3);
+          if (bad != 0)
+            for (int r = 0; r < kTile; r += 8)
+              if ((bad >> (r >> 3)) & 1u) clean(r, r + 8, true);
           if (any) misc[8 + (item & 7)] = item + 1;
           async_proxy_fence();
           __syncwarp();
@@ -914,44 +964,36 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         const int head = walk.kvh * p.group + row_head;
         uint8_t* out = p.out.data + 2 * ((int64_t)g.b * p.out.batch_stride + (int64_t)t * p.out.token_stride + (int64_t)head * p.out.head_stride);
         const int part_row = (PAIR ? slot * kTileRows : 0) + row;
-        const int h0 = PAIR ? 0 : slot * (D / 64), h1 = PAIR ? D / 32 : h0 + D / 64;  // the slots of one row tile share its columns
+        const int h0 = PAIR ? 0 : slot * (D / 32), h1 = PAIR ? D / 16 : h0 + D / 32;  // the slots of one row tile share its columns
 #pragma unroll 1
         for (int h = h0; h < h1; ++h) {
-          uint32_t x[32];
-          float o[32];
-          if (use0) {
-            tmem_ld32(tmem + lanes + 2 * kTile + (PAIR ? slot * 128 : 0) + h * 32, x);
+          uint32_t x[16], y[16];
+          float o[16];
+          if (use0) tmem_ask16(tmem + lanes + 2 * kTile + (PAIR ? slot * 128 : 0) + h * 16, x);
+          if (use1) tmem_ask16(tmem + lanes + 2 * kTile + 128 + h * 16, y);
+          tmem_wait16(x, y);
 #pragma unroll
-            for (int c = 0; c < 32; ++c) o[c] = __uint_as_float(x[c]) * w0;
-          } else {
-#pragma unroll
-            for (int c = 0; c < 32; ++c) o[c] = 0.f;
-          }
-          if (use1) {
-            tmem_ld32(tmem + lanes + 2 * kTile + 128 + h * 32, x);
-#pragma unroll
-            for (int c = 0; c < 32; ++c) o[c] = fmaf(__uint_as_float(x[c]), w1, o[c]);
-          }
+          for (int c = 0; c < 16; ++c) o[c] = (use0 ? __uint_as_float(x[c]) * w0 : 0.f) + (use1 ? __uint_as_float(y[c]) * w1 : 0.f);
           if (poison && live) {
-            float y[32];
+            float z[16];
 #pragma unroll
-            for (int c = 0; c < 32; ++c) y[c] = o[c];
-            add_back<E4M3>(p, g.b, walk.kvh, row_pos, g.lo_first, g.lo_last, min(g.L + g.t0 + 1, g.hi), g.hi, h * 32, y);
+            for (int c = 0; c < 16; ++c) z[c] = o[c];
+            add_back<E4M3>(p, g.b, walk.kvh, row_pos, g.lo_first, g.lo_last, min(g.L + g.t0 + 1, g.hi), g.hi, h * 16, z);
 #pragma unroll
-            for (int c = 0; c < 32; ++c) o[c] = y[c];
+            for (int c = 0; c < 16; ++c) o[c] = z[c];
           }
 #pragma unroll
-          for (int c = 0; c < 32; ++c) o[c] *= inv;
+          for (int c = 0; c < 16; ++c) o[c] *= inv;
           if (live) {
             if (whole) {
 #pragma unroll
-              for (int c = 0; c < 32; c += 8)
-                *reinterpret_cast<uint4*>(out + 2 * (h * 32 + c)) = make_uint4(cache::pack_bf16(o[c], o[c + 1]), cache::pack_bf16(o[c + 2], o[c + 3]),
+              for (int c = 0; c < 16; c += 8)
+                *reinterpret_cast<uint4*>(out + 2 * (h * 16 + c)) = make_uint4(cache::pack_bf16(o[c], o[c + 1]), cache::pack_bf16(o[c + 2], o[c + 3]),
                                                                                cache::pack_bf16(o[c + 4], o[c + 5]), cache::pack_bf16(o[c + 6], o[c + 7]));
             } else {
 #pragma unroll
-              for (int c = 0; c < 32; c += 4)
-                p.part_o[part_at<D, S::kItemRows>(blockIdx.x, from_start, h * 8 + c / 4, part_row)] = make_float4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+              for (int c = 0; c < 16; c += 4)
+                p.part_o[part_at<D, S::kItemRows>(blockIdx.x, from_start, h * 4 + c / 4, part_row)] = make_float4(o[c], o[c + 1], o[c + 2], o[c + 3]);
             }
           }
           __syncwarp();
