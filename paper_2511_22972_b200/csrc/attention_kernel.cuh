@@ -574,6 +574,14 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = misc[0];
+  // The lengths and a sequence's row of the block table are asked for in L2: a prefetch reads nothing for the program, so the kernel before may still
+  // be writing them.  (Which sequences a CTA will get is not known yet; as if all were as long.)
+  if (warp == S::kWarpV) {
+    const int b = (int)((int64_t)blockIdx.x * p.B / gridDim.x);
+    if (lane * 32 < p.B) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.c.lengths + lane * 32));
+    if (p.counts && lane * 32 < p.B) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.counts + lane * 32));
+    if (((int64_t)lane * 32 << p.c.page_shift) < p.c.capacity) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.c.table + b * p.c.table_stride + lane * 32));
+  }
   asm volatile("griddepcontrol.wait;" ::: "memory");  // everything below reads or writes what the kernels before may be working on
   asm volatile("griddepcontrol.launch_dependents;");
 

@@ -156,85 +156,132 @@ __device__ __forceinline__ uint32_t amax2(uint32_t a, uint32_t b) {  // of two p
   return __vmaxu2(a & 0x7fff7fffu, b & 0x7fff7fffu);
 }
 
-constexpr int kThreads = 256;
+// Threads of a block, and rows of a lane group taken together so that their loads are in flight together.  us, rows at a time: append 3 x 4099
+// tokens of 8 heads 1: 15.7 (blocks of 256 threads 16.8), 2: 19.7; read 8 x 4 - 16 k tokens 1: 102.4, 2: 101.9, 4: 96.1 (blocks of 128
+// threads 98.9), 8: 103.
+constexpr int kAppendThreads = 128, kReadThreads = 256, kAppendRows = 1, kReadRows = 4;
 
-// One group of D / 8 lanes per (sequence, token, head), eight values of the key and eight of the value per lane.
-template <int D, bool E4M3>
-__global__ void __launch_bounds__(kThreads) append_kernel(const View c, const Rows k, const Rows v, int B, int n, const int32_t* counts,
+// A group of D / 16 lanes per (sequence, token, head), sixteen values of the key and sixteen of the value per lane.  What bounds these kernels is
+// bytes, or for small calls the chain length -> page -> row.
+template <int D, bool E4M3, int ROWS>
+__global__ void __launch_bounds__(kAppendThreads) append_kernel(const View c, const Rows k, const Rows v, int B, int n, const int32_t* counts,
                                                           uint32_t* row_flags, int wide) {
-  constexpr int kLanes = D / 8;
+  constexpr int kLanes = D / 16, kGroups = kAppendThreads / kLanes;
   asm volatile("griddepcontrol.wait;" ::: "memory");  // the kernel before may have written any of the inputs
   asm volatile("griddepcontrol.launch_dependents;");
   const int lane = (int)threadIdx.x % kLanes;
-  const int64_t row = (int64_t)blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes;
-  if (row >= (int64_t)n * c.kv_heads) return;  // (whole groups)
-  const int i = (int)(row / c.kv_heads), head = (int)(row - (int64_t)i * c.kv_heads);
+  const uint32_t row0 = blockIdx.x * (kGroups * ROWS) + threadIdx.x / kLanes, rows = (uint32_t)n * (uint32_t)c.kv_heads;
+  const unsigned group = ((1u << kLanes) - 1u) << ((threadIdx.x & 31) / kLanes * kLanes);
   for (int b = (int)blockIdx.y; b < B; b += (int)gridDim.y) {
-    if (i >= count_of(counts, b, n)) continue;
-    const int L = length_of(c, b);
-    const int64_t pos = (int64_t)L + i;
-    const int page = L < 0 || pos >= c.capacity ? -1 : page_of(c, b, (int)pos);
-    if (row_flags && lane == 0 && head == 0) row_flags[(int64_t)b * n + i] = page < 0 ? kFlagNotWritten : 0u;
-    if (page < 0) continue;
-    const int slot = (int)pos & ((1 << c.page_shift) - 1);
+    const int count = count_of(counts, b, n), L = length_of(c, b);
+    uint4 x[ROWS][2][2];
+    int page[ROWS], token[ROWS], head[ROWS];
+    bool mine[ROWS];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const Rows& src = t ? v : k;
-      const uint4 x = load8(src.data + 2 * ((int64_t)b * src.batch_stride + (int64_t)i * src.token_stride + (int64_t)head * src.head_stride + lane * 8),
-                            (wide >> t) & 1);
-      uint8_t* pages = t ? c.v_pages : c.k_pages;
-      const int64_t at = row_at(c, page, slot, head) + lane * 8;
-      if (!E4M3) {
-        *reinterpret_cast<uint4*>(pages + 2 * at) = x;
-        continue;
+    for (int r = 0; r < ROWS; ++r) {  // (the rows need no page)
+      const uint32_t row = row0 + r * kGroups;
+      token[r] = (int)(row / (uint32_t)c.kv_heads);
+      head[r] = (int)(row - (uint32_t)token[r] * (uint32_t)c.kv_heads);
+      mine[r] = row < rows && token[r] < count;
+      if (!mine[r]) continue;
+      page[r] = L < 0 || (int64_t)L + token[r] >= c.capacity ? -1 : page_of(c, b, L + token[r]);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const Rows& src = t ? v : k;
+        const uint8_t* from = src.data + 2 * ((int64_t)b * src.batch_stride + (int64_t)token[r] * src.token_stride + (int64_t)head[r] * src.head_stride + lane * 16);
+        x[r][t][0] = load8(from, (wide >> t) & 1);
+        x[r][t][1] = load8(from + 16, (wide >> t) & 1);
       }
-      const uint32_t m2 = __vmaxu2(amax2(x.x, x.y), amax2(x.z, x.w));
-      uint32_t m = max(m2 & 0xffffu, m2 >> 16);
-      const unsigned group = (kLanes == 32 ? 0xffffffffu : ((1u << kLanes) - 1u) << ((threadIdx.x & 31) / kLanes * kLanes));
-      m = __reduce_max_sync(group, m);
-      const int s = scale_of(m);
-      const float inv = __uint_as_float((uint32_t)(254 - s) << 23);
-      uint2 codes = make_uint2(0u, 0u);
-      if (s != kScaleNan)
-        codes = make_uint2(pack_e4m3(bf16_lo(x.x) * inv, bf16_hi(x.x) * inv, bf16_lo(x.y) * inv, bf16_hi(x.y) * inv),
-                           pack_e4m3(bf16_lo(x.z) * inv, bf16_hi(x.z) * inv, bf16_lo(x.w) * inv, bf16_hi(x.w) * inv));
-      *reinterpret_cast<uint2*>(pages + at) = codes;
-      if (lane == 0) (t ? c.v_scales : c.k_scales)[scale_at(c, page, slot, head)] = (uint8_t)s;
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      if (!mine[r]) continue;  // (whole groups)
+      if (row_flags && lane == 0 && head[r] == 0) row_flags[(int64_t)b * n + token[r]] = page[r] < 0 ? kFlagNotWritten : 0u;
+      if (page[r] < 0) continue;
+      const int slot = (L + token[r]) & ((1 << c.page_shift) - 1);
+      const int64_t at = row_at(c, page[r], slot, head[r]) + lane * 16;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        uint8_t* pages = t ? c.v_pages : c.k_pages;
+        const uint4 y = x[r][t][0], z = x[r][t][1];
+        if (!E4M3) {
+          *reinterpret_cast<uint4*>(pages + 2 * at) = y;
+          *reinterpret_cast<uint4*>(pages + 2 * at + 16) = z;
+          continue;
+        }
+        const uint32_t m2 = __vmaxu2(__vmaxu2(amax2(y.x, y.y), amax2(y.z, y.w)), __vmaxu2(amax2(z.x, z.y), amax2(z.z, z.w)));
+        uint32_t m = max(m2 & 0xffffu, m2 >> 16);
+        m = __reduce_max_sync(group, m);
+        const int s = scale_of(m);
+        const float inv = __uint_as_float((uint32_t)(254 - s) << 23);
+        uint4 codes = make_uint4(0u, 0u, 0u, 0u);
+        if (s != kScaleNan)
+          codes = make_uint4(pack_e4m3(bf16_lo(y.x) * inv, bf16_hi(y.x) * inv, bf16_lo(y.y) * inv, bf16_hi(y.y) * inv),
+                             pack_e4m3(bf16_lo(y.z) * inv, bf16_hi(y.z) * inv, bf16_lo(y.w) * inv, bf16_hi(y.w) * inv),
+                             pack_e4m3(bf16_lo(z.x) * inv, bf16_hi(z.x) * inv, bf16_lo(z.y) * inv, bf16_hi(z.y) * inv),
+                             pack_e4m3(bf16_lo(z.z) * inv, bf16_hi(z.z) * inv, bf16_lo(z.w) * inv, bf16_hi(z.w) * inv));
+        *reinterpret_cast<uint4*>(pages + at) = codes;
+        if (lane == 0) (t ? c.v_scales : c.k_scales)[scale_at(c, page[r], slot, head[r])] = (uint8_t)s;
+      }
     }
   }
 }
 
-template <int D, bool E4M3>
-__global__ void __launch_bounds__(kThreads) read_kernel(const View c, const Rows k, const Rows v, int B, int n, const int32_t* starts, int wide) {
-  constexpr int kLanes = D / 8;
+// The same groups; a lane's sixteen values come as codes or as they are.
+template <int D, bool E4M3, int ROWS>
+__global__ void __launch_bounds__(kReadThreads) read_kernel(const View c, const Rows k, const Rows v, int B, int n, const int32_t* starts, int wide) {
+  constexpr int kLanes = D / 16, kGroups = kReadThreads / kLanes;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
   const int lane = (int)threadIdx.x % kLanes;
-  const int64_t row = (int64_t)blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes;
-  if (row >= (int64_t)n * c.kv_heads) return;
-  const int i = (int)(row / c.kv_heads), head = (int)(row - (int64_t)i * c.kv_heads);
+  const uint32_t row0 = blockIdx.x * (kGroups * ROWS) + threadIdx.x / kLanes, rows = (uint32_t)n * (uint32_t)c.kv_heads;
   for (int b = (int)blockIdx.y; b < B; b += (int)gridDim.y) {
-    const int64_t pos = (starts ? (int64_t)starts[b] : 0) + i;
-    if (pos < 0 || pos >= length_of(c, b)) continue;
-    const int page = page_of(c, b, (int)pos);
-    if (page < 0) continue;
-    const int slot = (int)pos & ((1 << c.page_shift) - 1);
+    const int64_t start = starts ? (int64_t)starts[b] : 0;
+    const int L = length_of(c, b);
+    int page[ROWS], token[ROWS], head[ROWS];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const uint8_t* pages = t ? c.v_pages : c.k_pages;
-      const int64_t at = row_at(c, page, slot, head) + lane * 8;
-      uint4 x;
-      if (E4M3) {
-        const uint2 codes = *reinterpret_cast<const uint2*>(pages + at);
-        const float scale = scale_value((t ? c.v_scales : c.k_scales)[scale_at(c, page, slot, head)]);
-        const uint2 a = values_e4m3(codes.x, scale), d = values_e4m3(codes.y, scale);
-        x = make_uint4(a.x, a.y, d.x, d.y);
-      } else {
-        x = *reinterpret_cast<const uint4*>(pages + 2 * at);
+    for (int r = 0; r < ROWS; ++r) {
+      const uint32_t row = row0 + r * kGroups;
+      token[r] = (int)(row / (uint32_t)c.kv_heads);
+      head[r] = (int)(row - (uint32_t)token[r] * (uint32_t)c.kv_heads);
+      const int64_t pos = start + token[r];
+      page[r] = row < rows && pos >= 0 && pos < L ? page_of(c, b, (int)pos) : -1;
+    }
+    uint4 x[ROWS][2][2];
+    int s[ROWS][2];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      if (page[r] < 0) continue;
+      const int slot = (int)(start + token[r]) & ((1 << c.page_shift) - 1);
+      const int64_t at = row_at(c, page[r], slot, head[r]) + lane * 16;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const uint8_t* pages = t ? c.v_pages : c.k_pages;
+        if (E4M3) {
+          x[r][t][0] = *reinterpret_cast<const uint4*>(pages + at);
+          s[r][t] = (t ? c.v_scales : c.k_scales)[scale_at(c, page[r], slot, head[r])];
+        } else {
+          x[r][t][0] = *reinterpret_cast<const uint4*>(pages + 2 * at);
+          x[r][t][1] = *reinterpret_cast<const uint4*>(pages + 2 * at + 16);
+        }
       }
-      const Rows& dst = t ? v : k;
-      store8(dst.data + 2 * ((int64_t)b * dst.batch_stride + (int64_t)i * dst.token_stride + (int64_t)head * dst.head_stride + lane * 8), x,
-             (wide >> t) & 1);
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      if (page[r] < 0) continue;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (E4M3) {
+          uint32_t w[8];
+          any16_e4m3(x[r][t][0], s[r][t], w);
+          x[r][t][0] = make_uint4(w[0], w[1], w[2], w[3]);
+          x[r][t][1] = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+        const Rows& dst = t ? v : k;
+        uint8_t* to = dst.data + 2 * ((int64_t)b * dst.batch_stride + (int64_t)token[r] * dst.token_stride + (int64_t)head[r] * dst.head_stride + lane * 16);
+        store8(to, x[r][t][0], (wide >> t) & 1);
+        store8(to + 16, x[r][t][1], (wide >> t) & 1);
+      }
     }
   }
 }

@@ -89,11 +89,14 @@ K::View view_of(const fly_cache_t* c) {
 
 K::Rows rows_of(const fly_rows_t* r) { return {static_cast<uint8_t*>(r->data), r->batch_stride, r->token_stride, r->head_stride}; }
 
-// One group of head_dim / 8 threads per (token, head), sequences along y.
-bool row_grid(const fly_cache_t* c, int32_t B, int32_t n, dim3* grid) {
-  const int64_t per_block = K::kThreads / (c->head_dim / 8), blocks = ((int64_t)n * c->kv_heads + per_block - 1) / per_block;
-  if (blocks > 0x7fffffff) return false;
-  *grid = dim3((unsigned)blocks, (unsigned)(B < 65535 ? B : 65535));
+// Groups of head_dim / 16 threads with one or `at_once` rows (tokens x heads) each, sequences along y.  Several rows at once where that still leaves
+// every SM its eight blocks.
+bool row_grid(const fly_cache_t* c, int32_t B, int32_t n, int threads, int at_once, dim3* grid, bool* several) {
+  const int64_t per_block = threads / (c->head_dim / 16), rows = (int64_t)n * c->kv_heads;
+  if (rows > 0x7fffff00) return false;  // (rows of a sequence are counted in 32 bits)
+  *several = at_once > 1 && (rows * B) / (per_block * at_once) >= 148 * 8;
+  const int64_t each = per_block * (*several ? at_once : 1);
+  *grid = dim3((unsigned)((rows + each - 1) / each), (unsigned)(B < 65535 ? B : 65535));
   return true;
 }
 
@@ -171,11 +174,15 @@ fly_status_t fly_cache_append(const fly_cache_t* c, int32_t B, int32_t n, const 
   if (!g.ok) return FLY_ERR_CUDA;
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute attr[1];
-  fill_launch(&cfg, attr, 1, K::kThreads, static_cast<cudaStream_t>(cuda_stream), true);
-  if (!row_grid(c, B, n, &cfg.gridDim)) return FLY_ERR_UNSUPPORTED;
+  fill_launch(&cfg, attr, 1, K::kAppendThreads, static_cast<cudaStream_t>(cuda_stream), true);
+  bool several;
+  if (!row_grid(c, B, n, K::kAppendThreads, K::kAppendRows, &cfg.gridDim, &several)) return FLY_ERR_UNSUPPORTED;
   const bool e4m3 = c->format == FLY_CACHE_E4M3;
-  auto kernel = c->head_dim == 128 ? (e4m3 ? K::append_kernel<128, true> : K::append_kernel<128, false>)
-                                   : (e4m3 ? K::append_kernel<64, true> : K::append_kernel<64, false>);
+  constexpr int R = K::kAppendRows;
+  auto kernel = c->head_dim == 128 ? (e4m3 ? (several ? K::append_kernel<128, true, R> : K::append_kernel<128, true, 1>)
+                                           : (several ? K::append_kernel<128, false, R> : K::append_kernel<128, false, 1>))
+                                   : (e4m3 ? (several ? K::append_kernel<64, true, R> : K::append_kernel<64, true, 1>)
+                                           : (several ? K::append_kernel<64, false, R> : K::append_kernel<64, false, 1>));
   const int aligned_rows = (wide(k, B, n, c->kv_heads) ? 1 : 0) | (wide(v, B, n, c->kv_heads) ? 2 : 0);
   return cudaLaunchKernelEx(&cfg, kernel, view_of(c), rows_of(k), rows_of(v), (int)B, (int)n, counts, row_flags, aligned_rows) == cudaSuccess
              ? FLY_OK
@@ -190,11 +197,15 @@ fly_status_t fly_cache_read(const fly_cache_t* c, int32_t B, int32_t n, const in
   if (!g.ok) return FLY_ERR_CUDA;
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute attr[1];
-  fill_launch(&cfg, attr, 1, K::kThreads, static_cast<cudaStream_t>(cuda_stream), true);
-  if (!row_grid(c, B, n, &cfg.gridDim)) return FLY_ERR_UNSUPPORTED;
+  fill_launch(&cfg, attr, 1, K::kReadThreads, static_cast<cudaStream_t>(cuda_stream), true);
+  bool several;
+  if (!row_grid(c, B, n, K::kReadThreads, K::kReadRows, &cfg.gridDim, &several)) return FLY_ERR_UNSUPPORTED;
   const bool e4m3 = c->format == FLY_CACHE_E4M3;
-  auto kernel = c->head_dim == 128 ? (e4m3 ? K::read_kernel<128, true> : K::read_kernel<128, false>)
-                                   : (e4m3 ? K::read_kernel<64, true> : K::read_kernel<64, false>);
+  constexpr int R = K::kReadRows;
+  auto kernel = c->head_dim == 128 ? (e4m3 ? (several ? K::read_kernel<128, true, R> : K::read_kernel<128, true, 1>)
+                                           : (several ? K::read_kernel<128, false, R> : K::read_kernel<128, false, 1>))
+                                   : (e4m3 ? (several ? K::read_kernel<64, true, R> : K::read_kernel<64, true, 1>)
+                                           : (several ? K::read_kernel<64, false, R> : K::read_kernel<64, false, 1>));
   const int aligned_rows = (wide(k, B, n, c->kv_heads) ? 1 : 0) | (wide(v, B, n, c->kv_heads) ? 2 : 0);
   return cudaLaunchKernelEx(&cfg, kernel, view_of(c), rows_of(k), rows_of(v), (int)B, (int)n, starts, aligned_rows) == cudaSuccess ? FLY_OK
                                                                                                                                   : FLY_ERR_CUDA;
