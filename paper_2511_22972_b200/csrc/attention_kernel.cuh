@@ -19,9 +19,14 @@
 // warp works its CTA's range out for itself.  Where a cut goes through an item its parts are left in scratch as (O, r, l) and
 // attention_combine_kernel adds them up, in a fixed order.
 //
-// Warps: 0-3 and 4-7 softmax of the two slots; one each for loading keys, values and queries by TMA into rings that run on across items, and
-// one that issues the MMAs; for E4M3 pages four more turn codes into the tiles of bf16 that the MMAs read (exactly: a code times a power of
-// two is a bf16 number).
+// E4M3.  The first product takes the keys' codes as they are (kind::f8f6f4) and the queries as the sum of an e4m3 and an e5m2 part: a bf16
+// has eight significant bits, four in the first part and what is left in at most three of the second, so a row scaled to the range
+// of e4m3 is exact down to 2^-17 of its largest value and off by 2^-22 of that below.  A token's key scale multiplies its column of
+// scores.  The values' codes become tiles of bf16 (exactly: a code times a power of two is a bf16 number), since weights cover far more
+// binades than 8 bits do.
+//
+// Warps: 0-3 and 4-7 softmax of the two slots (and, for E4M3, the queries' parts); one each for loading keys, values and queries by TMA into
+// rings that run on across items, and one that issues the MMAs; for E4M3 four more turn the values' codes into bf16.
 //
 // A value meets rows that must not see it with P = 0, and 0 * NaN is NaN.  In tiles where not every row of the item sees every position, the
 // values that no row sees are therefore zeroed in shared memory, and infinities and NaN in those that only some rows see are zeroed too
@@ -45,7 +50,7 @@ constexpr int kErrAttention = 5;
 
 struct Params {
   cache::View c;
-  cache::Rows out;
+  cache::Rows q, out;
   float* lse;
   const int32_t* counts;
   int B, n, heads, group;  // group: query heads per key/value head
@@ -127,6 +132,13 @@ __device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t a_hi,
       "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, p;\n\t}" ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+// The same for 8-bit floats.
+__device__ __forceinline__ void mma_ss8(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %4, p;\n\t}" ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
 // The same with A in tensor memory: lane = row, a 32-bit column = two consecutive entries of K.
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -186,6 +198,16 @@ __device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lbo_bytes) {
   return ((addr >> 4) & 0x3fffu) | (((lbo_bytes >> 4) & 0x3fffu) << 16);
 }
 __host__ __device__ constexpr uint32_t desc_hi(uint32_t group_bytes) { return (group_bytes >> 4) | (1u << 14) | (2u << 29); }
+// For rows of 64 bytes: 64-byte swizzle, groups of 8 rows 512 bytes apart.
+__host__ __device__ constexpr uint32_t desc_hi8(int D) { return D == 128 ? desc_hi(1024) : (512u >> 4) | (1u << 14) | (4u << 29); }
+// Place of 16-byte piece `piece` of row `row` in a tile of rows of D bytes.
+__device__ __forceinline__ int code_at(int D, int row, int piece) {
+  return D == 128 ? row * 128 + (((piece ^ row) & 7) << 4) : row * 64 + (((piece ^ (row >> 1)) & 3) << 4);
+}
+// fp32 accumulator, 8-bit A (e4m3, or e5m2) and B (e4m3), both K-major, M = 128.
+__host__ __device__ constexpr uint32_t instr_desc8(int n, bool a_e5m2) {
+  return (1u << 4) | ((a_e5m2 ? 1u : 0u) << 7) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);
+}
 // fp32 accumulator, bf16 A and B, A K-major, M = 128.
 __host__ __device__ constexpr uint32_t instr_desc(int n, bool b_mn_major) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);
@@ -195,28 +217,35 @@ __host__ __device__ constexpr uint32_t instr_desc(int n, bool b_mn_major) {
 
 template <int D, bool E4M3, bool PAIR>
 struct Shape {
-  // A tile of 128 rows: 64 values of eight rows are 1024 bytes, a swizzle atom.  Queries: one half (64 columns) of all rows after the other.
+  // A bf16 tile of 128 rows: 64 values of eight rows are 1024 bytes, a swizzle atom.  Queries: one half (64 columns) of all rows after the other.
   // Keys and values: eight rows after the other, both halves side by side, which is what one TMA box brings.
   static constexpr int kHalves = D / 64;
   static constexpr int kHalfBytes = 128 * 128;
   static constexpr int kGroupBytes = kHalves * 1024;        // eight rows of keys or values
   static constexpr int kTileBytes = kHalves * kHalfBytes;
-  static constexpr int kQBufs = PAIR || !E4M3 ? 2 : 1;      // (one row tile in two buffers: the next item's is loaded meanwhile)
-  static constexpr int kRawTile = kTile * D;                // a tile of codes
-  static constexpr int kRawBytes = kRawTile + kTile;        // ... and its scales
-  static constexpr int kStages = E4M3 ? (D == 128 ? (PAIR ? 3 : 4) : 6) : (D == 128 ? 5 : 12);
-  static constexpr int kRawStages = E4M3 ? (D == 128 ? 4 : 10) : 0;
+  static constexpr int kCodeBytes = kTile * D;              // a tile of codes
+  static constexpr int kQBufs = PAIR || !E4M3 ? 2 : 1;      // bf16 queries of one row tile: two buffers, the next item's come meanwhile
+  // Ring of keys (bf16, or codes), of values in bf16, and of values' codes with their scale bytes
+  static constexpr int kKBytes = E4M3 ? kCodeBytes : kTileBytes;
+  static constexpr int kKStages = E4M3 ? (D == 128 ? (PAIR ? 3 : 4) : 8) : (D == 128 ? 3 : 6);
+  static constexpr int kVStages = E4M3 ? (D == 128 ? 2 : 4) : (D == 128 ? 2 : 6);
+  static constexpr int kRawBytes = kCodeBytes + kTile;
+  static constexpr int kRawStages = E4M3 ? (D == 128 ? (PAIR ? 2 : 3) : 6) : 0;
+  static constexpr int kScaleRing = D == 128 ? 8 : 16;      // tiles whose key scales (fp32) are kept: two more than the ring of keys, and over
+  static_assert(kScaleRing >= kKStages + 2, "");
   static constexpr int kWarpK = 8, kWarpV = 9, kWarpMma = 10, kWarpQ = 11, kWarpConv = 12;
   static constexpr int kConvWarps = E4M3 ? 4 : 0, kConvThreads = kConvWarps * 32;
   static constexpr int kThreads = (kWarpConv + kConvWarps) * 32;
   static constexpr int kItemRows = PAIR ? 2 * kTileRows : kTileRows;
-  static constexpr int kOffRing = kQBufs * kTileBytes;
-  static constexpr int kOffRaw = kOffRing + kStages * kTileBytes;
-  static constexpr int kOffExchange = kOffRaw + kRawStages * kRawBytes;
+  static constexpr int kOffK = kQBufs * kTileBytes;         // (E4M3: both parts of a row tile's queries take what its bf16 would)
+  static constexpr int kOffV = kOffK + kKStages * kKBytes;
+  static constexpr int kOffRaw = kOffV + kVStages * kTileBytes;
+  static constexpr int kOffScales = kOffRaw + kRawStages * kRawBytes;
+  static constexpr int kOffExchange = kOffScales + (E4M3 ? (kScaleRing + 1) * kTile * 4 : 0);  // (the last one: ones)
   static constexpr int kOffBar = kOffExchange + 2 * kTileRows * 8;
-  static constexpr int kNumBars = 2 * kStages + 2 * kRawStages + 4 + 6;
+  static constexpr int kNumBars = 2 * kKStages + 2 * kVStages + 2 * kRawStages + 4 + 6;
   static constexpr int kOffFlags = kOffBar + kNumBars * 8;
-  static constexpr int kOffMisc = kOffFlags + 16 * 4;
+  static constexpr int kOffMisc = kOffFlags + 2 * 16 * 4;
   static constexpr int kSmem = kOffMisc + 64;
   static_assert(kSmem <= 232448, "shared memory of one CTA");
   // Place of 16-byte piece `piece` of row `row` in a tile of keys or values.
@@ -329,15 +358,6 @@ __device__ __forceinline__ bool slot_sees(const Params& p, const Group& g, int s
   if (ts0 >= ts1 || p0 >= g.L + ts1) return false;
   return p.window == 0 || p0 + kTile - 1 > g.L + ts0 - p.window || p0 < p.sinks;
 }
-// Places in the ring of an item's 2 m tiles: keys run ahead of values by as much as the MMAs do.
-template <bool PAIR>
-__device__ __forceinline__ int ring_k(int j) {
-  return PAIR ? 2 * j : j == 0 ? 0 : 2 * j - 1;
-}
-template <bool PAIR>
-__device__ __forceinline__ int ring_v(int j, int m) {
-  return PAIR ? 2 * j + 1 : j == m - 1 ? 2 * m - 1 : 2 * j + 2;
-}
 // 0: no row of the item sees position pos, 1: some do, 2: all.
 __device__ __forceinline__ int seen_by(const Params& p, const Group& g, int pos) {
   if (pos >= g.hi) return 0;
@@ -395,13 +415,30 @@ struct RowMask {
     return v;
   }
 };
-// Scores that a row does not see become -inf, in tensor memory, for tiles where there are any.  32 columns at a time in a loop: code that runs
-// once an item is fetched anew each time, about four cycles an instruction, and as part of the unrolled step below the mask took 4000 cycles.
-__device__ __forceinline__ void hide(uint32_t ts, const RowMask& mask) {
+// 32 scores times their keys' scales.
+__device__ __forceinline__ void scale32(uint32_t (&r)[32], const float* scales) {
+#pragma unroll
+  for (int c = 0; c < 32; c += 4) {
+    const float4 s = *reinterpret_cast<const float4*>(scales + c);
+    float x, y;
+    unpack2(mul2(pack2(__uint_as_float(r[c]), __uint_as_float(r[c + 1])), pack2(s.x, s.y)), x, y);
+    r[c] = __float_as_uint(x);
+    r[c + 1] = __float_as_uint(y);
+    unpack2(mul2(pack2(__uint_as_float(r[c + 2]), __uint_as_float(r[c + 3])), pack2(s.z, s.w)), x, y);
+    r[c + 2] = __float_as_uint(x);
+    r[c + 3] = __float_as_uint(y);
+  }
+}
+// Scores that a row does not see become -inf, in tensor memory, for tiles where there are any (E4M3: after the keys' scales, which may be NaN).  32
+// columns at a time in a loop: code that runs once an item is fetched anew each time, about four cycles an instruction, and as part
+// of the unrolled step below the mask took 4000 cycles.
+template <bool E4M3>
+__device__ __forceinline__ void hide(uint32_t ts, const RowMask& mask, const float* scales) {
   uint32_t r[32];
 #pragma unroll 1
   for (int c0 = 0; c0 < kTile; c0 += 32) {
     tmem_ld32(ts + c0, r);
+    if (E4M3) scale32(r, scales + c0);
     const uint32_t v = mask.bits(c0);
 #pragma unroll
     for (int c = 0; c < 32; ++c) r[c] = v & (1u << c) ? r[c] : 0xff800000u;
@@ -439,21 +476,32 @@ constexpr int kOffP = 64;  // P's first column over S: its columns are taken fro
 
 // One step of a row: S in tensor memory at `ts` becomes P there, the row's reference and sum move on, and O at `to` is rescaled if it must be.
 // Columns come 32 at a time, the next ones on their way while one block is worked on; the last block of the maximum is the
-// first of the exponentials.
-template <int D>
-__device__ __forceinline__ void softmax_step(uint32_t ts, uint32_t to, float scale, bool first, float& ref, float& sum) {
+// first of the exponentials.  E4M3: one block after the other, in loops: there are more warps with code of their own, and short loops spare
+// the instruction caches (16 sequences of nine over e4m3 189 -> 158 us; bf16 chunks of 2000 1003 -> 1045, so not there).
+template <int D, bool E4M3>
+__device__ __forceinline__ void softmax_step(uint32_t ts, uint32_t to, float scale, bool first, const float* scales, float& ref, float& sum) {
   uint32_t a[32], b[32];
-  tmem_ld32(ts, a);
-  tmem_ask32(ts + 32, b);
-  float mx = max32(a, -INFINITY);
-  tmem_wait(b);
-  tmem_ask32(ts + 64, a);
-  mx = max32(b, mx);
-  tmem_wait(a);
-  tmem_ask32(ts + 96, b);
-  mx = max32(a, mx);
-  tmem_wait(b);
-  mx = max32(b, mx);
+  float mx = -INFINITY;
+  if (E4M3) {
+#pragma unroll 1
+    for (int h = 0; h < 4; ++h) {
+      tmem_ld32(ts + h * 32, b);
+      scale32(b, scales + h * 32);
+      mx = max32(b, mx);
+    }
+  } else {
+    tmem_ld32(ts, a);
+    tmem_ask32(ts + 32, b);
+    mx = max32(a, mx);
+    tmem_wait(b);
+    tmem_ask32(ts + 64, a);
+    mx = max32(b, mx);
+    tmem_wait(a);
+    tmem_ask32(ts + 96, b);
+    mx = max32(a, mx);
+    tmem_wait(b);
+    mx = max32(b, mx);
+  }
   const float top = mx * scale;
   const bool move = top > ref + 8.0f;  // (false for a row that has seen nothing, and for NaN)
   if (__any_sync(0xffffffffu, move)) {
@@ -473,14 +521,25 @@ __device__ __forceinline__ void softmax_step(uint32_t ts, uint32_t to, float sca
   const float nr = ref == -INFINITY ? 0.f : -ref;
   const f2 sc2 = pack2(scale, scale), nr2 = pack2(nr, nr);
   f2 acc[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+  if (E4M3) {
 #pragma unroll 1
-  for (int h = 1; h >= 0; --h) {
-    tmem_ask32(ts + h * 64, a);
-    exp32(b, sc2, nr2, acc, ts + kOffP + h * 32 + 16);
-    tmem_wait(a);
-    if (h != 0) tmem_ask32(ts + 32, b);
-    exp32(a, sc2, nr2, acc, ts + kOffP + h * 32);
-    if (h != 0) tmem_wait(b);
+    for (int h = 3; h >= 0; --h) {
+      if (h < 3) {
+        tmem_ld32(ts + h * 32, b);
+        scale32(b, scales + h * 32);
+      }
+      exp32(b, sc2, nr2, acc, ts + kOffP + h * 16);
+    }
+  } else {
+#pragma unroll 1
+    for (int h = 1; h >= 0; --h) {
+      tmem_ask32(ts + h * 64, a);
+      exp32(b, sc2, nr2, acc, ts + kOffP + h * 32 + 16);
+      tmem_wait(a);
+      if (h != 0) tmem_ask32(ts + 32, b);
+      exp32(a, sc2, nr2, acc, ts + kOffP + h * 32);
+      if (h != 0) tmem_wait(b);
+    }
   }
   float x, y;
   unpack2(add2(acc[0], acc[1]), x, y);
@@ -534,18 +593,21 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t base = smem_u32(smem);
   const uint32_t bar0 = base + S::kOffBar;
-  auto full = [&](int s) { return bar0 + 8u * s; };                       // a stage's tile is there, in bf16
-  auto empty = [&](int s) { return bar0 + 8u * (S::kStages + s); };       // ... has been read by its MMAs
-  auto raw_full = [&](int s) { return bar0 + 8u * (2 * S::kStages + s); };
-  auto raw_empty = [&](int s) { return bar0 + 8u * (2 * S::kStages + S::kRawStages + s); };
-  constexpr int kB = 2 * S::kStages + 2 * S::kRawStages;
+  auto k_full = [&](uint32_t s) { return bar0 + 8u * s; };                 // a stage's tile is there
+  auto k_empty = [&](uint32_t s) { return bar0 + 8u * (S::kKStages + s); };  // ... has been read by its MMAs
+  auto v_full = [&](uint32_t s) { return bar0 + 8u * (2 * S::kKStages + s); };
+  auto v_empty = [&](uint32_t s) { return bar0 + 8u * (2 * S::kKStages + S::kVStages + s); };
+  auto raw_full = [&](uint32_t s) { return bar0 + 8u * (2 * S::kKStages + 2 * S::kVStages + s); };
+  auto raw_empty = [&](uint32_t s) { return bar0 + 8u * (2 * S::kKStages + 2 * S::kVStages + S::kRawStages + s); };
+  constexpr uint32_t kB = 2 * S::kKStages + 2 * S::kVStages + 2 * S::kRawStages, kRaw = E4M3 ? S::kRawStages : 1;
   auto q_full = [&](int s) { return bar0 + 8u * (kB + s); };
   auto q_empty = [&](int s) { return bar0 + 8u * (kB + 2 + s); };
   auto s_full = [&](int s) { return bar0 + 8u * (kB + 4 + s); };          // S of a slot's step is complete (and every MMA before it)
   auto p_ready = [&](int s) { return bar0 + 8u * (kB + 6 + s); };         // its P is there, O rescaled, the values' tile cleaned
   auto o_full = [&](int s) { return bar0 + 8u * (kB + 8 + s); };          // the slot's O of an item is complete
   volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(smem + S::kOffMisc);  // [0] tensor memory, [1] a role gave up, [8..15] items with values to add back
-  volatile uint32_t* tile_bad = reinterpret_cast<volatile uint32_t*>(smem + S::kOffFlags);  // of tile number t: entry t % 16
+  volatile uint32_t* tile_bad = reinterpret_cast<volatile uint32_t*>(smem + S::kOffFlags);  // of tile number t: entry t % 16, for the conversion 16 + t % 16
+  float* key_scales = reinterpret_cast<float*>(smem + S::kOffScales);  // of tile number t: entry t % kScaleRing
   float2* exchange = reinterpret_cast<float2*>(smem + S::kOffExchange);
 
   const int tid = (int)threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -553,16 +615,19 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
-    for (int s = 0; s < S::kStages; ++s) { mbar_init(full(s), E4M3 ? S::kConvThreads : 1); mbar_init(empty(s), 1); }
+    for (int s = 0; s < S::kKStages; ++s) { mbar_init(k_full(s), 1); mbar_init(k_empty(s), 1); }
+    for (int s = 0; s < S::kVStages; ++s) { mbar_init(v_full(s), E4M3 ? S::kConvThreads : 1); mbar_init(v_empty(s), 1); }
     for (int s = 0; s < S::kRawStages; ++s) { mbar_init(raw_full(s), 33); mbar_init(raw_empty(s), S::kConvThreads); }
     for (int s = 0; s < 2; ++s) {
-      mbar_init(q_full(s), 1);
+      mbar_init(q_full(s), E4M3 ? (PAIR ? kTileRows : 2 * kTileRows) : 1);
       mbar_init(q_empty(s), 1);
       mbar_init(s_full(s), 1);
       mbar_init(p_ready(s), kTileRows);
       mbar_init(o_full(s), 1);
     }
     misc[1] = 0;
+    if (E4M3)
+      for (int i = 0; i < kTile; ++i) key_scales[S::kScaleRing * kTile + i] = 1.f;
     for (int i = 8; i < 16; ++i) misc[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -589,74 +654,100 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
   // lanes decide alike.)
   bool failed = __shfl_sync(0xffffffffu, lane == 0 ? *reinterpret_cast<volatile int*>(p.status) : 0, 0) != 0;
   auto wait = [&](uint32_t bar, uint32_t parity) {
-    if (!failed && !mbar_wait(bar, parity, p.status, kErrAttention)) failed = true;
+    if (!failed && !mbar_wait_suspended(bar, parity, p.status, kErrAttention)) failed = true;
     __syncwarp();
   };
   auto wait_warp = [&](uint32_t bar, uint32_t parity) {  // the same decision in the whole warp
-    if (!failed && !__all_sync(0xffffffffu, mbar_wait(bar, parity, p.status, kErrAttention))) failed = true;
+    if (!failed && !__all_sync(0xffffffffu, mbar_wait_suspended(bar, parity, p.status, kErrAttention))) failed = true;
   };
   const Range range = range_of(p);
   Walk walk(p, range);
-  uint32_t ring = 0;     // tiles of keys and values that went through the ring before this item
-  uint32_t tile_no = 0;  // tiles of positions before this item
+  uint32_t tile_no = 0;  // tiles before this item: tile j of the item is in stage (tile_no + j) % stages of each ring
 
   if (warp >= 8 && warp < S::kWarpConv) {
   if (warp == S::kWarpK || warp == S::kWarpV) {
     // ---------------- keys, or values: a lane per box ----------------
     const bool values = warp == S::kWarpV;
     const int page_size = 1 << p.c.page_shift;
-    // E4M3: a box is a page's part of the tile, its scales follow with plain copies.  bf16: a box is eight rows with all their columns.
+    // E4M3: a box is a page's part of the tile.  bf16: a box is eight rows with all their columns.
     const int rows = E4M3 ? min(page_size, kTile) : 8;
     const uint32_t box_bytes = (uint32_t)rows * D * (E4M3 ? 1 : 2);
-    constexpr int kRing = E4M3 ? S::kRawStages : S::kStages;
+    const int of = E4M3 ? lane * rows >> 3 : lane;  // the group of eight whose page this lane's box is on
     for (; walk.have(); walk.next()) {
       const Group& g = walk.gr;
       const int m = walk.tiles();
-      int page = tile_page(p, g, walk.x0);
+      // Scales are asked for a tile ahead, pages two.  A lane has the scales of four (keys: as fp32) or eight (values) positions.
+      auto key_bytes = [&](int page, int p0) {
+        const int pg = __shfl_sync(0xffffffffu, page, lane >> 1);
+        return E4M3 && !values && pg >= 0
+                   ? *reinterpret_cast<const uint32_t*>(p.c.k_scales + cache::scale_at(p.c, pg, (p0 + 4 * lane) & (page_size - 1), walk.kvh))
+                   : 0u;
+      };
+      int page = tile_page(p, g, walk.x0), page1 = m > 1 ? tile_page(p, g, walk.x0 + 1) : -2;
+      uint32_t bytes = key_bytes(page, tile_start(g, walk.x0));
       for (int j = 0; j < m; ++j) {
-        const int ahead = j + 1 < m ? tile_page(p, g, walk.x0 + j + 1) : -2;
+        const int page2 = j + 2 < m ? tile_page(p, g, walk.x0 + j + 2) : -2;
         const int p0 = tile_start(g, walk.x0 + j);
-        if (!values) {  // what stands on a page that does not exist is not seen (read behind the keys' barrier)
-          const unsigned bad = __ballot_sync(0xffffffffu, page == -1) & 0xffffu;
-          if (lane == 0) tile_bad[(tile_no + (uint32_t)j) & 15] = bad;
+        const uint32_t bytes1 = j + 1 < m ? key_bytes(page1, tile_start(g, walk.x0 + j + 1)) : 0u;
+        const uint32_t no = tile_no + (uint32_t)j;
+        uint32_t there, dst;
+        // What stands on a page that does not exist is not seen.  (Read behind the barrier of the keys, or of the values' codes.)
+        const unsigned bad = __ballot_sync(0xffffffffu, page == -1) & 0xffffu;
+        if (!values) {
+          const uint32_t st = no % S::kKStages;
+          wait_warp(k_empty(st), ((no / S::kKStages) & 1) ^ 1);
+          there = k_full(st);
+          dst = base + S::kOffK + st * S::kKBytes;
+          if (lane == 0) tile_bad[no & 15] = bad;
+          if (E4M3)
+            *reinterpret_cast<float4*>(key_scales + (no % S::kScaleRing) * kTile + 4 * lane) =
+                make_float4(cache::scale_value(bytes & 255u), cache::scale_value((bytes >> 8) & 255u), cache::scale_value((bytes >> 16) & 255u), cache::scale_value(bytes >> 24));
+        } else if (E4M3) {
+          const uint32_t st = no % kRaw;
+          wait_warp(raw_empty(st), ((no / kRaw) & 1) ^ 1);
+          there = raw_full(st);
+          dst = base + S::kOffRaw + st * S::kRawBytes;
+          if (lane == 0) tile_bad[16 + (no & 15)] = bad;
+        } else {
+          const uint32_t st = no % S::kVStages;
+          wait_warp(v_empty(st), ((no / S::kVStages) & 1) ^ 1);
+          there = v_full(st);
+          dst = base + S::kOffV + st * S::kTileBytes;
         }
-        const uint32_t idx = ring + (uint32_t)(values ? ring_v<PAIR>(j, m) : ring_k<PAIR>(j));
-        const int st = (int)(idx % (uint32_t)kRing);
-        const uint32_t there = E4M3 ? raw_full(st) : full(st);
-        wait_warp(E4M3 ? raw_empty(st) : empty(st), ((idx / (uint32_t)kRing) & 1) ^ 1);
         if (failed) break;
-        const int of = E4M3 ? lane * rows >> 3 : lane;  // the group of eight whose page this lane's box is on
-        const int pg = __shfl_sync(0xffffffffu, page, of & 15);
-        const int at = p0 + 8 * of;
+        const int pg = __shfl_sync(0xffffffffu, page, of & 15), at = p0 + 8 * of;
         const bool mine = of < 16 && pg >= 0 && (E4M3 || at + 8 > g.lo_first || at < p.sinks);
         const unsigned have = __ballot_sync(0xffffffffu, mine);
+        __syncwarp();
         if (lane == 0) mbar_expect_tx(there, (uint32_t)__popc(have) * box_bytes);
         __syncwarp();
         const int slot = at & (page_size - 1);
         const CUtensorMap* map = values ? &map_v : &map_k;
         if (E4M3) {
-          const uint32_t dst = base + S::kOffRaw + st * S::kRawBytes;
           if (mine) tma_load_4d(dst + lane * rows * D, map, 0, slot, walk.kvh, pg, there);
-          // eight scales a lane, in the same phase of the barrier
-          if (lane < 16 && page >= 0) {
-            const uint8_t* s = (values ? p.c.v_scales : p.c.k_scales) + cache::scale_at(p.c, page, (p0 + 8 * lane) & (page_size - 1), walk.kvh);
-            asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst + S::kRawTile + lane * 8), "l"(s) : "memory");
+          if (values) {  // eight scales a lane, in the same phase of the barrier
+            if (lane < 16 && page >= 0)
+              asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst + S::kCodeBytes + lane * 8),
+                           "l"(p.c.v_scales + cache::scale_at(p.c, page, (p0 + 8 * lane) & (page_size - 1), walk.kvh))
+                           : "memory");
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(there) : "memory");
           }
-          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(there) : "memory");
         } else if (mine) {
-          tma_load_5d(base + S::kOffRing + st * S::kTileBytes + lane * S::kGroupBytes, map, 0, slot, 0, walk.kvh, pg, there);
+          tma_load_5d(dst + lane * S::kGroupBytes, map, 0, slot, 0, walk.kvh, pg, there);
         }
         __syncwarp();
-        page = ahead;
+        page = page1;
+        page1 = page2;
+        bytes = bytes1;
       }
       if (failed) break;
-      ring += 2u * m;
       tile_no += m;
     }
   } else if (warp == S::kWarpQ) {
     // ---------------- queries: (heads of the group, tokens) boxes; tokens behind the chunk's end come as zeros ----------------
+    // (E4M3: the softmax warps take the queries apart themselves)
     uint32_t item = 0;
-    for (; walk.have(); walk.next(), ++item) {
+    for (; !E4M3 && walk.have(); walk.next(), ++item) {
       for (int s = 0; s < (PAIR ? 2 : 1); ++s) {
         const int buf = PAIR ? s : (int)(item % S::kQBufs);
         wait_warp(q_empty(buf), ((PAIR ? item : item / S::kQBufs) & 1) ^ 1);
@@ -696,14 +787,21 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       const int m = walk.tiles();
       auto sees = [&](int s, int j) { return !PAIR || slot_sees(p, g, s, tile_start(g, walk.x0 + j)); };
       auto issue_s = [&](int s, int j) {  // S of slot s = Q x keys of tile j
-        const uint32_t st = (ring + (uint32_t)ring_k<PAIR>(j)) % S::kStages;
+        const uint32_t st = (tile_no + (uint32_t)j) % S::kKStages;
         const int buf = PAIR ? s : (int)(item % S::kQBufs);
         if (!failed && lead) {
-          const uint32_t a = desc_lo(base + buf * S::kTileBytes, 16), b = desc_lo(base + S::kOffRing + st * S::kTileBytes, 16);
+          const uint32_t a = desc_lo(base + buf * S::kTileBytes, 16), b = desc_lo(base + S::kOffK + st * S::kKBytes, 16);
+          if (E4M3) {
 #pragma unroll
-          for (int k = 0; k < D / 16; ++k)
-            mma_ss(tmem + s * kTile, a + ((uint32_t)((k / 4) * S::kHalfBytes + (k % 4) * 32) >> 4), desc_hi(1024),
-                   b + ((uint32_t)((k / 4) * 1024 + (k % 4) * 32) >> 4), desc_hi(S::kGroupBytes), kIdescS, k != 0);
+            for (int k = 0; k < D / 32; ++k) mma_ss8(tmem + s * kTile, a + k * 2, b + k * 2, desc_hi8(D), instr_desc8(kTile, false), k != 0);
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) mma_ss8(tmem + s * kTile, a + (S::kCodeBytes >> 4) + k * 2, b + k * 2, desc_hi8(D), instr_desc8(kTile, true), 1);
+          } else {
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+              mma_ss(tmem + s * kTile, a + ((uint32_t)((k / 4) * S::kHalfBytes + (k % 4) * 32) >> 4), desc_hi(1024),
+                     b + ((uint32_t)((k / 4) * 1024 + (k % 4) * 32) >> 4), desc_hi(S::kGroupBytes), kIdescS, k != 0);
+          }
           mma_commit(s_full(s));
         }
         __syncwarp();
@@ -712,10 +810,10 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         uint32_t& use = s ? use1 : use0;
         wait_warp(p_ready(s), use & 1);
         ++use;
-        const uint32_t st = (ring + (uint32_t)ring_v<PAIR>(j, m)) % S::kStages;
+        const uint32_t st = (tile_no + (uint32_t)j) % S::kVStages;
         tc_fence_after();
         if (!failed && lead) {
-          const uint32_t b = desc_lo(base + S::kOffRing + st * S::kTileBytes, 1024);
+          const uint32_t b = desc_lo(base + S::kOffV + st * S::kTileBytes, 1024);
           const uint32_t to = tmem + 2 * kTile + s * 128, from = tmem + s * kTile + kOffP;
           const Span span = tile_span(p, g, tile_start(g, walk.x0 + j));
           if (span.first == 0 && span.last == kTile) {
@@ -731,15 +829,20 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         }
         __syncwarp();
       };
-      auto wait_tile = [&](int place) {
-        const uint32_t idx = ring + (uint32_t)place;
-        wait_warp(full((int)(idx % S::kStages)), (idx / S::kStages) & 1);
+      auto wait_k = [&](int j) {
+        const uint32_t no = tile_no + (uint32_t)j;
+        wait_warp(k_full(no % S::kKStages), (no / S::kKStages) & 1);
+      };
+      auto wait_v = [&](int j) {
+        const uint32_t no = tile_no + (uint32_t)j;
+        wait_warp(v_full(no % S::kVStages), (no / S::kVStages) & 1);
       };
       auto commit = [&](uint32_t bar) {
         if (!failed && lead) mma_commit(bar);
         __syncwarp();
       };
-      auto release = [&](int place) { commit(empty((int)((ring + (uint32_t)place) % S::kStages))); };
+      auto release_k = [&](int j) { commit(k_empty((tile_no + (uint32_t)j) % S::kKStages)); };
+      auto release_v = [&](int j) { commit(v_empty((tile_no + (uint32_t)j) % S::kVStages)); };
       if (PAIR) {
         wait_warp(q_full(0), item & 1);
         wait_warp(q_full(1), item & 1);
@@ -748,12 +851,12 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
           if (g.t0 + s * p.tpt < g.t1)
             for (last[s] = m - 1; last[s] >= 0 && !sees(s, last[s]); --last[s]) {}
         bool begun[2] = {false, false};
-        wait_tile(ring_k<PAIR>(0));
+        wait_k(0);
         for (int s = 0; s < 2; ++s)
           if (sees(s, 0)) issue_s(s, 0);
-        release(ring_k<PAIR>(0));
+        release_k(0);
         for (int j = 0; j < m; ++j) {
-          wait_tile(ring_v<PAIR>(j, m));
+          wait_v(j);
           for (int s = 0; s < 2; ++s) {
             if (sees(s, j)) {
               issue_o(s, j, begun[s]);
@@ -761,35 +864,37 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
               if (j == last[s]) commit(o_full(s));
             }
             if (j + 1 < m) {
-              if (s == 0) wait_tile(ring_k<PAIR>(j + 1));
+              if (s == 0) wait_k(j + 1);
               if (sees(s, j + 1)) issue_s(s, j + 1);
             }
           }
-          release(ring_v<PAIR>(j, m));
-          if (j + 1 < m) release(ring_k<PAIR>(j + 1));
+          release_v(j);
+          if (j + 1 < m) release_k(j + 1);
         }
-        commit(q_empty(0));
-        commit(q_empty(1));
+        if (!E4M3) {
+          commit(q_empty(0));
+          commit(q_empty(1));
+        }
       } else {
         const int buf = (int)(item % S::kQBufs);
         wait_warp(q_full(buf), (item / S::kQBufs) & 1);
         auto scores = [&](int j) {
-          wait_tile(ring_k<PAIR>(j));
+          wait_k(j);
           issue_s(j & 1, j);
-          release(ring_k<PAIR>(j));
-          if (j == m - 1) commit(q_empty(buf));
+          release_k(j);
+          if (!E4M3 && j == m - 1) commit(q_empty(buf));
         };
         scores(0);
         if (m > 1) scores(1);
         for (int j = 0; j < m; ++j) {
-          wait_tile(ring_v<PAIR>(j, m));
+          wait_v(j);
           issue_o(j & 1, j, j >= 2);
-          release(ring_v<PAIR>(j, m));
+          release_v(j);
           if (j + 2 >= m) commit(o_full(j & 1));
           if (j + 2 < m) scores(j + 2);
         }
       }
-      ring += 2u * m;
+      tile_no += m;
     }
     if (failed && lead) {  // what has been issued ends before shared and tensor memory are given back
       mma_commit(q_full(0));
@@ -811,29 +916,27 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     for (; walk.have(); walk.next(), ++item) {
       const Group& g = walk.gr;
       const int m = walk.tiles();
-      auto convert = [&](int place, bool values, int j) {
-        const uint32_t idx = ring + (uint32_t)place;
-        constexpr uint32_t kRing = S::kRawStages > 0 ? S::kRawStages : 1;
-        const int rs = (int)(idx % kRing), st = (int)(idx % S::kStages);
-        wait_warp(raw_full(rs), (idx / kRing) & 1);
-        wait_warp(empty(st), ((idx / S::kStages) & 1) ^ 1);
+      for (int j = 0; j < m; ++j) {
+        const uint32_t no = tile_no + (uint32_t)j, rs = no % kRaw, st = no % S::kVStages;
+        wait_warp(raw_full(rs), (no / kRaw) & 1);
+        wait_warp(v_empty(st), ((no / S::kVStages) & 1) ^ 1);
         const uint8_t* raw = smem + S::kOffRaw + rs * S::kRawBytes;
-        uint8_t* dst = smem + S::kOffRing + st * S::kTileBytes;
+        uint8_t* dst = smem + S::kOffV + st * S::kTileBytes;
         const int p0 = tile_start(g, walk.x0 + j);
-        const uint32_t bad = tile_bad[(tile_no + (uint32_t)j) & 15];
-        const bool edge = values && (bad != 0 || tile_unseen(p, g, p0) || tile_partial(p, g, p0));
+        const uint32_t bad = tile_bad[16 + (no & 15)];
+        const bool edge = bad != 0 || tile_unseen(p, g, p0) || tile_partial(p, g, p0);
         bool any = false;
-#pragma unroll
+#pragma unroll 1
         for (int i0 = 0; i0 < kEach; i0 += 4) {
           uint4 codes[4];
           int scale[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             codes[i] = *reinterpret_cast<const uint4*>(raw + from0 + (i0 + i) * kRowStep * D);
-            scale[i] = raw[S::kRawTile + row0 + (i0 + i) * kRowStep];
+            scale[i] = raw[S::kCodeBytes + row0 + (i0 + i) * kRowStep];
           }
           uint32_t w[4][8];
-          if (!cache::plain4_e4m3(codes, scale)) {
+          if (!cache::plain_e4m3<4>(codes, scale)) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) cache::any16_e4m3(codes[i], scale[i], w[i]);
           } else {
@@ -857,16 +960,11 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         if (any) misc[8 + (item & 7)] = item + 1;
         async_proxy_fence();
         if (!failed) {
-          mbar_arrive(full(st));
+          mbar_arrive(v_full(st));
           mbar_arrive(raw_empty(rs));
         }
         __syncwarp();
-      };
-      for (int j = 0; j <= m; ++j) {  // K(0) [V(0)] K(1) V(0 or 1) ...
-        if (j < m) convert(ring_k<PAIR>(j), false, j);
-        if (PAIR ? j < m : j > 0) convert(ring_v<PAIR>(PAIR ? j : j - 1, m), true, PAIR ? j : j - 1);
       }
-      ring += 2u * m;
       tile_no += m;
     }
   } else {
@@ -884,8 +982,51 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       const bool live = row_token < p.tpt && t < ts1;
       const bool warp_live = __any_sync(0xffffffffu, live);
       const int first_hi = min(g.L + ts0 + 1, g.hi), last_lo = p.window > 0 ? g.L + ts1 - p.window : 0;
-      float ref = -INFINITY, sum = 0.f;
+      float ref = -INFINITY, sum = 0.f, scale = p.scale;
       bool begun = false;
+      if (E4M3) {
+        // The row's queries in two parts (of one row tile: both slots take half of the columns).  Every MMA that read the item before's is done: its O was
+        // waited for.
+        constexpr int kPieces = PAIR ? D / 8 : D / 16;  // of eight values
+        const int piece0 = PAIR ? 0 : slot * kPieces;
+        const bool there = row_token < p.tpt && t < p.n;
+        const uint4* from = reinterpret_cast<const uint4*>(p.q.data + 2 * ((int64_t)g.b * p.q.batch_stride + (int64_t)t * p.q.token_stride +
+                                                                           (int64_t)(walk.kvh * p.group + row_head) * p.q.head_stride)) + piece0;
+        uint32_t m2 = 0u;
+        if (there) {
+#pragma unroll 4
+          for (int i = 0; i < kPieces; ++i) {
+            const uint4 v = from[i];
+            m2 = __vmaxu2(m2, __vmaxu2(cache::amax2(v.x, v.y), cache::amax2(v.z, v.w)));
+          }
+        }
+        uint32_t amax = max(m2 & 0xffffu, m2 >> 16);
+        if (!PAIR) {
+          exchange[slot * kTileRows + row].x = __uint_as_float(amax);
+          asm volatile("bar.sync 1, 256;" ::: "memory");
+          amax = max(amax, __float_as_uint(exchange[(slot ^ 1) * kTileRows + row].x));
+        }
+        const int s = cache::scale_of(amax);
+        scale *= cache::scale_value(s);  // (NaN: the row is)
+        const float inv = s == cache::kScaleNan ? 0.f : __uint_as_float((uint32_t)(254 - s) << 23);
+        uint8_t* hi = smem + (PAIR ? slot * S::kTileBytes : 0);
+#pragma unroll 1
+        for (int i = 0; i < kPieces; i += 2) {  // 16 values: 16 bytes of each part
+          uint32_t w[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+          if (there && s != cache::kScaleNan) {
+            const uint4 u = from[i], v = from[i + 1];
+            const uint32_t x[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int c = 0; c < 8; c += 2) cache::split_e4m3_e5m2(x[c], x[c + 1], inv, w[c / 2], w[4 + c / 2]);
+          }
+          const int at = code_at(D, row, (piece0 + i) / 2);
+          *reinterpret_cast<uint4*>(hi + at) = make_uint4(w[0], w[1], w[2], w[3]);
+          *reinterpret_cast<uint4*>(hi + S::kCodeBytes + at) = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+        async_proxy_fence();
+        mbar_arrive(q_full(PAIR ? slot : 0));
+        if (!PAIR) asm volatile("bar.sync 1, 256;" ::: "memory");  // (the exchange is used again at the item's end)
+      }
       for (int j = PAIR ? 0 : slot; j < m; j += PAIR ? 1 : 2) {
         const int p0 = tile_start(g, walk.x0 + j);
         if (PAIR && !slot_sees(p, g, slot, p0)) continue;
@@ -900,18 +1041,19 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             mask.lim = min(row_pos + 1, g.hi) - p0;
             mask.lo = p.window > 0 ? row_pos + 1 - p.window - p0 : 0;
             mask.snk = p.sinks - p0;
-            hide(ts, mask);
+            hide<E4M3>(ts, mask, key_scales + ((tile_no + (uint32_t)j) % S::kScaleRing) * kTile);
+            softmax_step<D, E4M3>(ts, to, scale, !begun, key_scales + S::kScaleRing * kTile, ref, sum);
+          } else {
+            softmax_step<D, E4M3>(ts, to, scale, !begun, key_scales + ((tile_no + (uint32_t)j) % S::kScaleRing) * kTile, ref, sum);
           }
-          softmax_step<D>(ts, to, p.scale, !begun, ref, sum);
           tmem_st_wait();
           tc_fence_before();
         }
         if (!E4M3 && (bad != 0 || tile_unseen(p, g, p0) || tile_partial(p, g, p0)) && (!PAIR || slot == 0 || !slot_sees(p, g, 0, p0))) {
           // The values' tile before its MMAs (those of both slots come after this slot's p_ready), 16 bytes at a time: only what the MMAs take.
-          const uint32_t idx = ring + (uint32_t)ring_v<PAIR>(j, m);
-          const int st = (int)(idx % S::kStages);
-          wait(full(st), (idx / S::kStages) & 1);
-          uint8_t* tile = smem + S::kOffRing + st * S::kTileBytes;
+          const uint32_t no = tile_no + (uint32_t)j, st = no % S::kVStages;
+          wait(v_full(st), (no / S::kVStages) & 1);
+          uint8_t* tile = smem + S::kOffV + st * S::kTileBytes;
           const Span span = tile_span(p, g, p0);
           bool any = false;
           auto clean = [&](int from, int to_row, bool zero) {  // rows from .. to_row - 1
@@ -1015,7 +1157,6 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         tc_fence_before();
       }
       if (!PAIR) asm volatile("bar.sync 1, 256;" ::: "memory");  // neither slot's O is overwritten before both have read it
-      ring += 2u * m;
       tile_no += m;
     }
   }

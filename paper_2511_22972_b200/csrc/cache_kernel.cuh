@@ -87,6 +87,18 @@ __device__ __forceinline__ void unpack_e4m3(uint16_t w, float& lo, float& hi) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(w));
   asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}" : "=f"(lo), "=f"(hi) : "r"(h));
 }
+// Four bf16 times inv as four e4m3 codes, and what is left of them as four e5m2 codes.
+__device__ __forceinline__ void split_e4m3_e5m2(uint32_t a, uint32_t b, float inv, uint32_t& hi, uint32_t& lo) {
+  const float x[4] = {bf16_lo(a) * inv, bf16_hi(a) * inv, bf16_lo(b) * inv, bf16_hi(b) * inv};
+  hi = pack_e4m3(x[0], x[1], x[2], x[3]);
+  float y[4];
+  unpack_e4m3((uint16_t)hi, y[0], y[1]);
+  unpack_e4m3((uint16_t)(hi >> 16), y[2], y[3]);
+  uint16_t u, v;
+  asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(u) : "f"(x[1] - y[1]), "f"(x[0] - y[0]));
+  asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(v) : "f"(x[3] - y[3]), "f"(x[2] - y[2]));
+  lo = (uint32_t)u | ((uint32_t)v << 16);
+}
 // Four codes as two pairs of bf16, scaled.
 __device__ __forceinline__ uint2 values_e4m3(uint32_t codes, float scale) {
   float a, b, c, d;
@@ -97,15 +109,18 @@ __device__ __forceinline__ uint2 values_e4m3(uint32_t codes, float scale) {
 
 // Sixteen codes as eight pairs of bf16, scaled, for where conversions are what there is to do.  Placed into a bf16's bits (sign, then exponent and
 // mantissa four places lower) a code reads as its value times 2^-120, subnormal codes as subnormal bf16; one multiplication by
-// 2^(s - 7) puts both right.  Not so for scales above 134 and for code 0x7f (NaN, which append never writes): plain4_e4m3 says whether
-// 4 x 16 codes are without, and any16_e4m3 takes all.
-__device__ __forceinline__ bool plain4_e4m3(const uint4 (&c)[4], const int (&s)[4]) {
-  uint32_t nan = 0u;
+// 2^(s - 7) puts both right.  Not so for scales above 134 and for code 0x7f (NaN, which append never writes): plain_e4m3 says whether
+// N x 16 codes are without, and any16_e4m3 takes all.
+template <int N>
+__device__ __forceinline__ bool plain_e4m3(const uint4 (&c)[N], const int (&s)[N]) {
+  uint32_t nan = 0u;  // (a byte 0x7f or 0xff changes its upper bit when one is added; others only by the carry of one of these)
+  int top = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    nan |= ((c[i].x & 0x7f7f7f7fu) + 0x01010101u) | ((c[i].y & 0x7f7f7f7fu) + 0x01010101u) | ((c[i].z & 0x7f7f7f7fu) + 0x01010101u) |
-           ((c[i].w & 0x7f7f7f7fu) + 0x01010101u);
-  return (nan & 0x80808080u) == 0u && max(max(s[0], s[1]), max(s[2], s[3])) <= 134;
+  for (int i = 0; i < N; ++i) {
+    nan |= ((c[i].x + 0x01010101u) ^ c[i].x) | ((c[i].y + 0x01010101u) ^ c[i].y) | ((c[i].z + 0x01010101u) ^ c[i].z) | ((c[i].w + 0x01010101u) ^ c[i].w);
+    top = max(top, s[i]);
+  }
+  return (nan & 0x80808080u) == 0u && top <= 134;
 }
 __device__ __forceinline__ void plain16_e4m3(const uint4& codes, int s, uint32_t (&w)[8]) {
   const uint32_t c[4] = {codes.x, codes.y, codes.z, codes.w}, f = (uint32_t)(s + 120) * 0x00800080u;  // 2^(s - 7) twice

@@ -124,8 +124,9 @@ bool encode_q(fly_attention* h, CUtensorMap* map, const fly_rows_t* q, const A::
                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Pages.  bf16: boxes of eight tokens with all their values, 64 at a time and swizzled.  E4M3: boxes of a page's (or 128) tokens' codes as they lie.
-bool encode_pages(fly_attention* h, CUtensorMap* map, const fly_cache_t* c, void* pages) {
+// Pages.  bf16: boxes of eight tokens with all their values, 64 at a time and swizzled.  E4M3: boxes of a page's (or 128) tokens' codes; keys swizzled, values as they lie.
+bool encode_pages(fly_attention* h, CUtensorMap* map, const fly_cache_t* c, bool keys) {
+  void* const pages = keys ? c->k_pages : c->v_pages;
   const bool e4m3 = c->format == FLY_CACHE_E4M3;
   const cuuint64_t D = (cuuint64_t)c->head_dim, esz = e4m3 ? 1 : 2;
   const cuuint64_t token = (cuuint64_t)c->token_stride * esz;
@@ -136,7 +137,8 @@ bool encode_pages(fly_attention* h, CUtensorMap* map, const fly_cache_t* c, void
     const cuuint64_t dims[4] = {D, tokens, heads, count}, bytes[3] = {token, head, page};
     const cuuint32_t box[4] = {(cuuint32_t)D, (cuuint32_t)(c->page_size < A::kTile ? c->page_size : A::kTile), 1, 1};
     return h->encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, pages, dims, bytes, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                           CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                           !keys ? CU_TENSOR_MAP_SWIZZLE_NONE : D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
   }
   const cuuint64_t dims[5] = {64, tokens, D / 64, heads, count}, bytes[4] = {token, 128, head, page};
   const cuuint32_t box[5] = {64, 8, (cuuint32_t)(D / 64), 1, 1};
@@ -275,6 +277,7 @@ fly_status_t fly_attention_run(fly_attention_t* h, const fly_cache_t* c, const f
   if (!g.ok) return FLY_ERR_CUDA;
   A::Params p;
   p.c = view_of(c);
+  p.q = rows_of(&a->q);
   p.out = rows_of(&a->out);
   p.lse = a->lse;
   p.counts = a->counts;
@@ -303,7 +306,7 @@ fly_status_t fly_attention_run(fly_attention_t* h, const fly_cache_t* c, const f
   p.status = h->status;
   const bool e4m3 = c->format == FLY_CACHE_E4M3;
   CUtensorMap maps[3];
-  if (!encode_q(h, &maps[0], &a->q, p) || !encode_pages(h, &maps[1], c, c->k_pages) || !encode_pages(h, &maps[2], c, c->v_pages))
+  if (!encode_q(h, &maps[0], &a->q, p) || !encode_pages(h, &maps[1], c, true) || !encode_pages(h, &maps[2], c, false))
     return FLY_ERR_UNSUPPORTED;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   h->last_launches = 0;
