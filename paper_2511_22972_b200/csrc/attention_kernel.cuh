@@ -60,7 +60,7 @@ struct Params {
   int tpi;                 // tokens per item
   int rt;                  // items per sequence and key/value head
   int groups;              // B * rt
-  int min_share;           // a CTA that gets work gets at least so many tiles
+  int item_cost;           // tiles that an item counts for besides its own: what it takes a CTA to change to it
   float4* part_o;          // [grid][2][D / 4][rows of an item]
   float2* part_ml;         // [grid][2][rows of an item]: r, l
   int* desc;               // [grid][8]: how a CTA's range begins
@@ -226,7 +226,7 @@ struct Shape {
   static constexpr int kCodeBytes = kTile * D;              // a tile of codes
   static constexpr int kQBufs = PAIR || !E4M3 ? 2 : 1;      // bf16 queries of one row tile: two buffers, the next item's come meanwhile
   // Ring of keys (bf16, or codes), of values in bf16, and of values' codes with their scale bytes
-  static constexpr int kKBytes = E4M3 ? kCodeBytes : kTileBytes;
+  static constexpr int kKBytes = E4M3 ? kCodeBytes : kTileBytes;  // (the scale bytes of a stage of codes lie by the fp32 ones)
   static constexpr int kKStages = E4M3 ? (D == 128 ? (PAIR ? 3 : 4) : 8) : (D == 128 ? 3 : 6);
   static constexpr int kVStages = E4M3 ? (D == 128 ? 2 : 4) : (D == 128 ? 2 : 6);
   static constexpr int kRawBytes = kCodeBytes + kTile;
@@ -241,9 +241,9 @@ struct Shape {
   static constexpr int kOffV = kOffK + kKStages * kKBytes;
   static constexpr int kOffRaw = kOffV + kVStages * kTileBytes;
   static constexpr int kOffScales = kOffRaw + kRawStages * kRawBytes;
-  static constexpr int kOffExchange = kOffScales + (E4M3 ? (kScaleRing + 1) * kTile * 4 : 0);  // (the last one: ones)
+  static constexpr int kOffExchange = kOffScales + (E4M3 ? (kScaleRing + 1) * kTile * 4 + kKStages * kTile : 0);  // fp32, ones, bytes by stage
   static constexpr int kOffBar = kOffExchange + 2 * kTileRows * 8;
-  static constexpr int kNumBars = 2 * kKStages + 2 * kVStages + 2 * kRawStages + 4 + 6;
+  static constexpr int kNumBars = 3 * kKStages + 2 * kVStages + 2 * kRawStages + 4 + 6;
   static constexpr int kOffFlags = kOffBar + kNumBars * 8;
   static constexpr int kOffMisc = kOffFlags + 2 * 16 * 4;
   static constexpr int kSmem = kOffMisc + 64;
@@ -254,7 +254,9 @@ struct Shape {
   }
 };
 
-// What a CTA takes of the items' tiles: `tiles` of them from place `off` of group g on.
+// The index space that is cut: every item's tiles, behind item_cost places where nothing lies.
+__device__ __forceinline__ int work_of(const Params& p, const Group& g) { return g.count > 0 ? (g.count + p.item_cost) * p.c.kv_heads : 0; }
+// What a CTA takes of it: `tiles` places from place `off` of group g on.
 struct Range {
   int share, tiles, off, g;
   Group gr;  // of g
@@ -263,10 +265,10 @@ __device__ __forceinline__ Range range_of(const Params& p) {  // (the host has s
   const int lane = (int)threadIdx.x & 31;
   Range r;
   Group g0 = group_at(p, min(lane, p.groups - 1));
-  const int count0 = lane < p.groups ? g0.count * p.c.kv_heads : 0;
+  const int count0 = lane < p.groups ? work_of(p, g0) : 0;
   int sum = count0;
 #pragma unroll 4
-  for (int g = 32 + lane; g < p.groups; g += 32) sum += group_at(p, g).count * p.c.kv_heads;
+  for (int g = 32 + lane; g < p.groups; g += 32) sum += work_of(p, group_at(p, g));
   int x0 = count0;  // over the first 32 groups
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -279,7 +281,7 @@ __device__ __forceinline__ Range range_of(const Params& p) {  // (the host has s
   } else {
     sum = __shfl_sync(0xffffffffu, x0, 31);
   }
-  r.share = max(p.min_share, (int)(((uint32_t)sum + gridDim.x - 1u) / gridDim.x));
+  r.share = max(1, (int)(((uint32_t)sum + gridDim.x - 1u) / gridDim.x));
   const uint32_t begin = (uint32_t)r.share * blockIdx.x;  // (at most sum + grid)
   r.g = r.off = r.tiles = 0;
   if (begin >= (uint32_t)sum) return r;
@@ -288,7 +290,7 @@ __device__ __forceinline__ Range range_of(const Params& p) {  // (the host has s
   int run = 0;
   for (int base = 0;; base += 32) {
     if (base > 0) g0 = group_at(p, min(base + lane, p.groups - 1));
-    const int v = base == 0 ? count0 : base + lane < p.groups ? g0.count * p.c.kv_heads : 0;
+    const int v = base == 0 ? count0 : base + lane < p.groups ? work_of(p, g0) : 0;
     int x = x0;
     if (base > 0) {
       x = v;
@@ -319,7 +321,7 @@ __device__ __forceinline__ Range range_of(const Params& p) {  // (the host has s
   }
 }
 
-// A role's walk over the items of its CTA's range.
+// A role's walk over the items of its CTA's range: tiles x0 .. x1 - 1 of item (g, kvh).
 struct Walk {
   const Params& p;
   int g, kvh, x0, x1, left;
@@ -327,28 +329,31 @@ struct Walk {
   __device__ __forceinline__ Walk(const Params& pp, const Range& r) : p(pp), g(r.g), kvh(0), x0(0), x1(0), left(r.tiles) {
     if (left > 0) {
       gr = r.gr;
-      kvh = (int)((uint32_t)r.off / (uint32_t)gr.count);
-      x0 = r.off - kvh * gr.count;
-      x1 = min(gr.count, x0 + left);
+      const int per = gr.count + p.item_cost;
+      kvh = (int)((uint32_t)r.off / (uint32_t)per);
+      begin(r.off - kvh * per);
     }
   }
-  __device__ __forceinline__ bool have() const { return left > 0; }
+  // The item from place `at` on.  (Where the range ends before its first tile the next CTA begins it.)
+  __device__ __forceinline__ void begin(int at) {
+    const int end = min(gr.count + p.item_cost, at + left);
+    left -= end - at;
+    x0 = max(0, at - p.item_cost);
+    x1 = end - p.item_cost;
+  }
+  __device__ __forceinline__ bool have() const { return x1 > x0; }
   __device__ __forceinline__ int tiles() const { return x1 - x0; }
   __device__ __forceinline__ void next() {
-    left -= x1 - x0;
+    x1 = x0;
     if (left <= 0) return;
-    x0 = 0;
     if (++kvh == p.c.kv_heads) {
       kvh = 0;
       do {
-        if (++g >= p.groups) {  // (does not happen: the tiles are counted alike)
-          left = 0;
-          return;
-        }
+        if (++g >= p.groups) return;  // (does not happen: the places are counted alike)
         gr = group_at(p, g);
       } while (gr.count == 0);
     }
-    x1 = min(gr.count, left);
+    begin(0);
   }
 };
 
@@ -391,13 +396,6 @@ __device__ __forceinline__ uint32_t zero_nonfinite(uint32_t w, bool& any) {  // 
   if ((w & 0x7f80u) == 0x7f80u) { w &= 0xffff0000u; any = true; }
   if ((w & 0x7f800000u) == 0x7f800000u) { w &= 0xffffu; any = true; }
   return w;
-}
-
-// The pages of a tile: lane l < 16 has that of its positions 8 l .. 8 l + 7.  -1: there is none, -2: they lie behind what is seen.
-__device__ __forceinline__ int tile_page(const Params& p, const Group& g, int x) {
-  const int lane = (int)threadIdx.x & 31, pos = tile_start(g, x) + 8 * lane;
-  if (lane >= 16 || pos >= g.hi) return -2;
-  return cache::page_of(p.c, g.b, pos);
 }
 
 __device__ __forceinline__ uint32_t below(int n) {  // the first n of 32 bits
@@ -600,6 +598,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
   auto raw_full = [&](uint32_t s) { return bar0 + 8u * (2 * S::kKStages + 2 * S::kVStages + s); };
   auto raw_empty = [&](uint32_t s) { return bar0 + 8u * (2 * S::kKStages + 2 * S::kVStages + S::kRawStages + s); };
   constexpr uint32_t kB = 2 * S::kKStages + 2 * S::kVStages + 2 * S::kRawStages, kRaw = E4M3 ? S::kRawStages : 1;
+  auto k_ready = [&](uint32_t s) { return E4M3 ? bar0 + 8u * (kB + 10 + s) : k_full(s); };  // ... and for E4M3 its keys' scales are in fp32
   auto q_full = [&](int s) { return bar0 + 8u * (kB + s); };
   auto q_empty = [&](int s) { return bar0 + 8u * (kB + 2 + s); };
   auto s_full = [&](int s) { return bar0 + 8u * (kB + 4 + s); };          // S of a slot's step is complete (and every MMA before it)
@@ -608,6 +607,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
   volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(smem + S::kOffMisc);  // [0] tensor memory, [1] a role gave up, [8..15] items with values to add back
   volatile uint32_t* tile_bad = reinterpret_cast<volatile uint32_t*>(smem + S::kOffFlags);  // of tile number t: entry t % 16, for the conversion 16 + t % 16
   float* key_scales = reinterpret_cast<float*>(smem + S::kOffScales);  // of tile number t: entry t % kScaleRing
+  uint8_t* key_bytes = smem + S::kOffScales + (S::kScaleRing + 1) * kTile * 4;
   float2* exchange = reinterpret_cast<float2*>(smem + S::kOffExchange);
 
   const int tid = (int)threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -615,7 +615,11 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
-    for (int s = 0; s < S::kKStages; ++s) { mbar_init(k_full(s), 1); mbar_init(k_empty(s), 1); }
+    for (int s = 0; s < S::kKStages; ++s) {
+      mbar_init(k_full(s), E4M3 ? 33 : 1);
+      mbar_init(k_empty(s), 1);
+      if (E4M3) mbar_init(k_ready(s), 1);
+    }
     for (int s = 0; s < S::kVStages; ++s) { mbar_init(v_full(s), E4M3 ? S::kConvThreads : 1); mbar_init(v_empty(s), 1); }
     for (int s = 0; s < S::kRawStages; ++s) { mbar_init(raw_full(s), 33); mbar_init(raw_empty(s), S::kConvThreads); }
     for (int s = 0; s < 2; ++s) {
@@ -676,79 +680,91 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     for (; walk.have(); walk.next()) {
       const Group& g = walk.gr;
       const int m = walk.tiles();
-      // Scales are asked for a tile ahead, pages two.  A lane has the scales of four (keys: as fp32) or eight (values) positions.
-      auto key_bytes = [&](int page, int p0) {
-        const int pg = __shfl_sync(0xffffffffu, page, lane >> 1);
-        return E4M3 && !values && pg >= 0
-                   ? *reinterpret_cast<const uint32_t*>(p.c.k_scales + cache::scale_at(p.c, pg, (p0 + 4 * lane) & (page_size - 1), walk.kvh))
-                   : 0u;
+      // The pages of several tiles come in one load, a lane each, and those of the next tiles are asked for when these begin to be used.
+      const int per_tile = max(0, 7 - p.c.page_shift), tiles_at_once = 32 >> per_tile;  // log2 of the pages of a tile
+      auto ask = [&](int j) {
+        const int tile = j + (lane >> per_tile), pos = tile < m ? tile_start(g, walk.x0 + tile) + ((lane & ((1 << per_tile) - 1)) << p.c.page_shift) : g.hi;
+        return pos < g.hi ? p.c.table[(int64_t)g.b * p.c.table_stride + (pos >> p.c.page_shift)] : -1;
       };
-      int page = tile_page(p, g, walk.x0), page1 = m > 1 ? tile_page(p, g, walk.x0 + 1) : -2;
-      uint32_t bytes = key_bytes(page, tile_start(g, walk.x0));
+      int pages = ask(0), pages_ahead = -1;
       for (int j = 0; j < m; ++j) {
-        const int page2 = j + 2 < m ? tile_page(p, g, walk.x0 + j + 2) : -2;
-        const int p0 = tile_start(g, walk.x0 + j);
-        const uint32_t bytes1 = j + 1 < m ? key_bytes(page1, tile_start(g, walk.x0 + j + 1)) : 0u;
-        const uint32_t no = tile_no + (uint32_t)j;
-        uint32_t there, dst;
+        const int in = j & (tiles_at_once - 1);
+        if (in == 0) {
+          if (j > 0) pages = pages_ahead;
+          pages_ahead = ask(j + tiles_at_once);
+        }
+        const int p0 = tile_start(g, walk.x0 + j), pos = p0 + 8 * lane;
+        int page = __shfl_sync(0xffffffffu, pages, (in << per_tile) + ((lane & 15) * 8 >> min(7, p.c.page_shift)));  // of eight positions
+        const bool need = lane < 16 && pos < g.hi;
         // What stands on a page that does not exist is not seen.  (Read behind the barrier of the keys, or of the values' codes.)
-        const unsigned bad = __ballot_sync(0xffffffffu, page == -1) & 0xffffu;
+        const unsigned bad = __ballot_sync(0xffffffffu, need && (page < 0 || page >= p.c.num_pages));
+        if (!need || ((bad >> lane) & 1u)) page = -1;
+        const uint32_t no = tile_no + (uint32_t)j;
+        uint32_t there, dst, bytes;
         if (!values) {
           const uint32_t st = no % S::kKStages;
           wait_warp(k_empty(st), ((no / S::kKStages) & 1) ^ 1);
           there = k_full(st);
           dst = base + S::kOffK + st * S::kKBytes;
+          bytes = smem_u32(key_bytes) + st * kTile;
           if (lane == 0) tile_bad[no & 15] = bad;
-          if (E4M3)
-            *reinterpret_cast<float4*>(key_scales + (no % S::kScaleRing) * kTile + 4 * lane) =
-                make_float4(cache::scale_value(bytes & 255u), cache::scale_value((bytes >> 8) & 255u), cache::scale_value((bytes >> 16) & 255u), cache::scale_value(bytes >> 24));
         } else if (E4M3) {
           const uint32_t st = no % kRaw;
           wait_warp(raw_empty(st), ((no / kRaw) & 1) ^ 1);
           there = raw_full(st);
           dst = base + S::kOffRaw + st * S::kRawBytes;
+          bytes = dst + S::kCodeBytes;
           if (lane == 0) tile_bad[16 + (no & 15)] = bad;
         } else {
           const uint32_t st = no % S::kVStages;
           wait_warp(v_empty(st), ((no / S::kVStages) & 1) ^ 1);
           there = v_full(st);
           dst = base + S::kOffV + st * S::kTileBytes;
+          bytes = 0;
         }
         if (failed) break;
-        const int pg = __shfl_sync(0xffffffffu, page, of & 15), at = p0 + 8 * of;
+        const int pg = E4M3 ? __shfl_sync(0xffffffffu, page, of & 15) : page, at = p0 + 8 * of;
         const bool mine = of < 16 && pg >= 0 && (E4M3 || at + 8 > g.lo_first || at < p.sinks);
         const unsigned have = __ballot_sync(0xffffffffu, mine);
-        __syncwarp();
         if (lane == 0) mbar_expect_tx(there, (uint32_t)__popc(have) * box_bytes);
         __syncwarp();
         const int slot = at & (page_size - 1);
         const CUtensorMap* map = values ? &map_v : &map_k;
         if (E4M3) {
+          if (page >= 0)  // eight scales a lane, in the same phase of the barrier
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(bytes + lane * 8),
+                         "l"((values ? p.c.v_scales : p.c.k_scales) + cache::scale_at(p.c, page, pos & (page_size - 1), walk.kvh))
+                         : "memory");
+          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(there) : "memory");
           if (mine) tma_load_4d(dst + lane * rows * D, map, 0, slot, walk.kvh, pg, there);
-          if (values) {  // eight scales a lane, in the same phase of the barrier
-            if (lane < 16 && page >= 0)
-              asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst + S::kCodeBytes + lane * 8),
-                           "l"(p.c.v_scales + cache::scale_at(p.c, page, (p0 + 8 * lane) & (page_size - 1), walk.kvh))
-                           : "memory");
-            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(there) : "memory");
-          }
         } else if (mine) {
           tma_load_5d(dst + lane * S::kGroupBytes, map, 0, slot, 0, walk.kvh, pg, there);
         }
         __syncwarp();
-        page = page1;
-        page1 = page2;
-        bytes = bytes1;
       }
       if (failed) break;
       tile_no += m;
     }
   } else if (warp == S::kWarpQ) {
     // ---------------- queries: (heads of the group, tokens) boxes; tokens behind the chunk's end come as zeros ----------------
-    // (E4M3: the softmax warps take the queries apart themselves)
+    // E4M3: the softmax warps take the queries apart themselves, and this one turns the keys' scale bytes into fp32, four a lane.
     uint32_t item = 0;
-    for (; !E4M3 && walk.have(); walk.next(), ++item) {
-      for (int s = 0; s < (PAIR ? 2 : 1); ++s) {
+    for (; walk.have(); walk.next(), ++item) {
+      if (E4M3) {
+        const int m = walk.tiles();
+        for (int j = 0; j < m; ++j) {
+          const uint32_t no = tile_no + (uint32_t)j, st = no % S::kKStages;
+          wait_warp(k_full(st), (no / S::kKStages) & 1);
+          const uint32_t b = *reinterpret_cast<const uint32_t*>(key_bytes + st * kTile + 4 * lane);
+          *reinterpret_cast<float4*>(key_scales + (no % S::kScaleRing) * kTile + 4 * lane) =
+              make_float4(cache::scale_value(b & 255u), cache::scale_value((b >> 8) & 255u), cache::scale_value((b >> 16) & 255u), cache::scale_value(b >> 24));
+          __syncwarp();
+          if (!failed && lane == 0) mbar_arrive(k_ready(st));
+          __syncwarp();
+        }
+        tile_no += m;
+      }
+      for (int s = 0; s < (E4M3 ? 0 : PAIR ? 2 : 1); ++s) {
         const int buf = PAIR ? s : (int)(item % S::kQBufs);
         wait_warp(q_empty(buf), ((PAIR ? item : item / S::kQBufs) & 1) ^ 1);
         if (!failed && elect_lane()) {
@@ -774,7 +790,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     // ---------------- MMA issue ----------------
     if (lane == 0) {  // how this CTA's range begins, for the kernel that adds up
       int4* d = reinterpret_cast<int4*>(p.desc) + 2 * blockIdx.x;
-      const bool any = range.tiles > 0;
+      const bool any = walk.have();
       d[0] = make_int4(any ? walk.x0 : 0, any ? walk.gr.count : 0, range.share, any ? walk.kvh : 0);
       d[1] = any ? make_int4(walk.gr.b, walk.gr.t0, walk.gr.t1, 0) : make_int4(0, 0, 0, 0);
     }
@@ -831,7 +847,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       };
       auto wait_k = [&](int j) {
         const uint32_t no = tile_no + (uint32_t)j;
-        wait_warp(k_full(no % S::kKStages), (no / S::kKStages) & 1);
+        wait_warp(k_ready(no % S::kKStages), (no / S::kKStages) & 1);
       };
       auto wait_v = [&](int j) {
         const uint32_t no = tile_no + (uint32_t)j;
@@ -994,6 +1010,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                                                                            (int64_t)(walk.kvh * p.group + row_head) * p.q.head_stride)) + piece0;
         uint32_t m2 = 0u;
         if (there) {
+          if (walk.kvh + 1 < p.c.kv_heads && p.q.head_stride > 0)  // the next item's, in all likelihood
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(from + (int64_t)p.group * p.q.head_stride / 8));
 #pragma unroll 4
           for (int i = 0; i < kPieces; ++i) {
             const uint4 v = from[i];
