@@ -256,9 +256,12 @@ struct Shape {
 
 // The index space that is cut: every item's tiles, behind item_cost places where nothing lies.
 __device__ __forceinline__ int work_of(const Params& p, const Group& g) { return g.count > 0 ? (g.count + p.item_cost) * p.c.kv_heads : 0; }
+// Few short items go to a CTA each: up to so many tiles take one CTA less than adding up parts does (9 tokens of 64 heads over 300 positions 12.3 ->
+// see the table of cases).
+constexpr int kWholeItem = 4;
 // What a CTA takes of it: `tiles` places from place `off` of group g on.
 struct Range {
-  int share, tiles, off, g;
+  int share, tiles, off, g, item_cost;  // item_cost < 0: whole items, a place each
   Group gr;  // of g
 };
 __device__ __forceinline__ Range range_of(const Params& p) {  // (the host has seen to it that all tiles together are fewer than 2^31)
@@ -282,6 +285,14 @@ __device__ __forceinline__ Range range_of(const Params& p) {  // (the host has s
     sum = __shfl_sync(0xffffffffu, x0, 31);
   }
   r.share = max(1, (int)(((uint32_t)sum + gridDim.x - 1u) / gridDim.x));
+  r.item_cost = p.item_cost;
+  if (p.groups <= 32 && p.groups * p.c.kv_heads <= (int)gridDim.x && __all_sync(0xffffffffu, g0.count <= kWholeItem)) {
+    const unsigned some = __ballot_sync(0xffffffffu, count0 > 0);
+    sum = __popc(some) * p.c.kv_heads;
+    x0 = __popc(some & (0xffffffffu >> (31 - lane))) * p.c.kv_heads;
+    r.share = 1;
+    r.item_cost = -1;
+  }
   const uint32_t begin = (uint32_t)r.share * blockIdx.x;  // (at most sum + grid)
   r.g = r.off = r.tiles = 0;
   if (begin >= (uint32_t)sum) return r;
@@ -290,7 +301,7 @@ __device__ __forceinline__ Range range_of(const Params& p) {  // (the host has s
   int run = 0;
   for (int base = 0;; base += 32) {
     if (base > 0) g0 = group_at(p, min(base + lane, p.groups - 1));
-    const int v = base == 0 ? count0 : base + lane < p.groups ? work_of(p, g0) : 0;
+    const int v = base == 0 ? (r.item_cost < 0 ? min(count0, p.c.kv_heads) : count0) : base + lane < p.groups ? work_of(p, g0) : 0;
     int x = x0;
     if (base > 0) {
       x = v;
@@ -324,22 +335,27 @@ __device__ __forceinline__ Range range_of(const Params& p) {  // (the host has s
 // A role's walk over the items of its CTA's range: tiles x0 .. x1 - 1 of item (g, kvh).
 struct Walk {
   const Params& p;
-  int g, kvh, x0, x1, left;
+  int g, kvh, x0, x1, left, item_cost;
   Group gr;
-  __device__ __forceinline__ Walk(const Params& pp, const Range& r) : p(pp), g(r.g), kvh(0), x0(0), x1(0), left(r.tiles) {
+  __device__ __forceinline__ Walk(const Params& pp, const Range& r) : p(pp), g(r.g), kvh(0), x0(0), x1(0), left(r.tiles), item_cost(r.item_cost) {
     if (left > 0) {
       gr = r.gr;
-      const int per = gr.count + p.item_cost;
+      const int per = item_cost < 0 ? 1 : gr.count + item_cost;
       kvh = (int)((uint32_t)r.off / (uint32_t)per);
       begin(r.off - kvh * per);
     }
   }
   // The item from place `at` on.  (Where the range ends before its first tile the next CTA begins it.)
   __device__ __forceinline__ void begin(int at) {
-    const int end = min(gr.count + p.item_cost, at + left);
+    if (item_cost < 0) {
+      left -= 1;
+      x1 = gr.count;
+      return;
+    }
+    const int end = min(gr.count + item_cost, at + left);
     left -= end - at;
-    x0 = max(0, at - p.item_cost);
-    x1 = end - p.item_cost;
+    x0 = max(0, at - item_cost);
+    x1 = end - item_cost;
   }
   __device__ __forceinline__ bool have() const { return x1 > x0; }
   __device__ __forceinline__ int tiles() const { return x1 - x0; }
@@ -1202,57 +1218,85 @@ __global__ void attention_selftest_kernel(int* status, unsigned long long limit_
   mbar_wait(b, 0, status, kErrAttention, limit_ns);
 }
 
-// Adds up the parts of the items that were cut: block x takes the item that CTA x + 1 of the main kernel went on with, if CTA x began it.
+// Adds up the parts of the items that were cut: those that CTA c went on with and CTA c - 1 began.
 //   r = max r_i,  l = sum 2^(r_i - r) l_i,  out = sum 2^(r_i - r) O_i / l
-// A lane per row, a warp per four columns.
+// Every block first lists them, so that there is no block without work but for the last ones (a block for every CTA that might have cut one took
+// 5 us where none had).  Then a thread takes four columns of a row, neighbouring threads neighbouring rows.
+constexpr int kCombineThreads = 256;
 template <int D, int ROWS>
-__global__ void __launch_bounds__(D * 8) attention_combine_kernel(const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(kCombineThreads) attention_combine_kernel(const __grid_constant__ Params p, int ctas) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
-  const int c = (int)blockIdx.x + 1, lane = (int)threadIdx.x & 31, col4 = (int)threadIdx.x >> 5;
-  const int4* d = reinterpret_cast<const int4*>(p.desc) + 2 * c;
-  const int4 a = d[0], e = d[1];
-  const int x0 = a.x, count = a.y, share = a.z, kvh = a.w, b = e.x, t0 = e.y, t1 = e.z;
-  if (x0 <= 0 || x0 > share) return;
-  const int parts = 1 + (count - x0 + share - 1) / share;
-  const int row = (int)blockIdx.y * 32 + lane, slot = row / kTileRows, in_slot = row - slot * kTileRows, token = in_slot / p.group;
-  const int t = t0 + slot * p.tpt + token;
-  if (token >= p.tpt || t >= t1) return;
-  float r = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  constexpr int kAtOnce = 4;
-  for (int i0 = 0; i0 < parts; i0 += kAtOnce) {
-    float2 ml[kAtOnce];
-    float4 x[kAtOnce];
-#pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
-      const int i = min(i0 + k, parts - 1);
-      ml[k] = p.part_ml[((int64_t)(c - 1 + i) * 2 + (i == 0 ? 1 : 0)) * ROWS + row];
-      x[k] = p.part_o[part_at<D, ROWS>(c - 1 + i, i == 0, col4, row)];
+  __shared__ int4 list[kCombineThreads][2];
+  __shared__ int in_warp[kCombineThreads / 32];
+  const int lane = (int)threadIdx.x & 31, warp = (int)threadIdx.x >> 5;
+  const int4* desc = reinterpret_cast<const int4*>(p.desc);
+  for (int c0 = 1; c0 < ctas; c0 += kCombineThreads) {  // (once, unless there are more SMs than threads)
+    const int mine = c0 + (int)threadIdx.x;
+    const int4 d = mine < ctas ? desc[2 * mine] : make_int4(0, 0, 0, 0);
+    int4 d1 = mine < ctas ? desc[2 * mine + 1] : make_int4(0, 0, 0, 0);
+    d1.w = mine;
+    const bool is = d.x > 0 && d.x <= d.z;
+    const unsigned others = __ballot_sync(0xffffffffu, is);
+    if (lane == 0) in_warp[warp] = __popc(others);
+    __syncthreads();
+    int cut = 0, before = __popc(others & ((1u << lane) - 1u));
+    for (int w = 0; w < kCombineThreads / 32; ++w) {
+      if (w < warp) before += in_warp[w];
+      cut += in_warp[w];
     }
-    float top = r;
-#pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) top = fmaxf(top, ml[k].x);
-    const float rr = top == -INFINITY ? 0.f : top, w0 = ex2_approx(r - rr);
-    r = top;
-    l *= w0;
-#pragma unroll
-    for (int v = 0; v < 4; ++v) o[v] *= w0;
-#pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
-      if (i0 + k >= parts) break;
-      const float w = ex2_approx(ml[k].x - rr);
-      l = fmaf(ml[k].y, w, l);
-      o[0] = fmaf(x[k].x, w, o[0]);
-      o[1] = fmaf(x[k].y, w, o[1]);
-      o[2] = fmaf(x[k].z, w, o[2]);
-      o[3] = fmaf(x[k].w, w, o[3]);
+    if (is) {  // (in the same order in every block)
+      list[before][0] = d;
+      list[before][1] = d1;
     }
+    __syncthreads();
+    const int rows = ROWS > kTileRows ? ROWS : p.tpt * p.group, per_item = rows * (D / 4);
+    for (int64_t u = (int64_t)blockIdx.x * kCombineThreads + threadIdx.x; u < (int64_t)cut * per_item; u += (int64_t)gridDim.x * kCombineThreads) {
+      const int k = (int)(u / per_item), in = (int)(u - (int64_t)k * per_item), col4 = in / rows, row = in - col4 * rows;
+      const int4 a = list[k][0], e = list[k][1];
+      const int c = e.w, x0 = a.x, count = a.y, share = a.z, kvh = a.w, b = e.x, t0 = e.y, t1 = e.z;
+      const int parts = 1 + (count - x0 + share - 1) / share;
+      const int slot = row / kTileRows, in_slot = row - slot * kTileRows, token = in_slot / p.group;
+      const int t = t0 + slot * p.tpt + token;
+      if (token >= p.tpt || t >= t1) continue;
+      float r = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+      constexpr int kAtOnce = 8;
+      for (int i0 = 0; i0 < parts; i0 += kAtOnce) {
+        float2 ml[kAtOnce];
+        float4 x[kAtOnce];
+#pragma unroll
+        for (int k2 = 0; k2 < kAtOnce; ++k2) {
+          const int i = min(i0 + k2, parts - 1);
+          ml[k2] = p.part_ml[((int64_t)(c - 1 + i) * 2 + (i == 0 ? 1 : 0)) * ROWS + row];
+          x[k2] = p.part_o[part_at<D, ROWS>(c - 1 + i, i == 0, col4, row)];
+        }
+        float top = r;
+#pragma unroll
+        for (int k2 = 0; k2 < kAtOnce; ++k2) top = fmaxf(top, ml[k2].x);
+        const float rr = top == -INFINITY ? 0.f : top, w0 = ex2_approx(r - rr);
+        r = top;
+        l *= w0;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) o[v] *= w0;
+#pragma unroll
+        for (int k2 = 0; k2 < kAtOnce; ++k2) {
+          if (i0 + k2 >= parts) break;
+          const float w = ex2_approx(ml[k2].x - rr);
+          l = fmaf(ml[k2].y, w, l);
+          o[0] = fmaf(x[k2].x, w, o[0]);
+          o[1] = fmaf(x[k2].y, w, o[1]);
+          o[2] = fmaf(x[k2].z, w, o[2]);
+          o[3] = fmaf(x[k2].w, w, o[3]);
+        }
+      }
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const int head = kvh * p.group + in_slot - token * p.group;
+      uint8_t* out = p.out.data + 2 * ((int64_t)b * p.out.batch_stride + (int64_t)t * p.out.token_stride + (int64_t)head * p.out.head_stride + col4 * 4);
+      *reinterpret_cast<uint2*>(out) = make_uint2(cache::pack_bf16(o[0] * inv, o[1] * inv), cache::pack_bf16(o[2] * inv, o[3] * inv));
+      if (p.lse && col4 == 0) p.lse[((int64_t)b * p.n + t) * p.heads + head] = l == 0.f ? -INFINITY : kLn2 * (r + log2f(l));
+    }
+    __syncthreads();
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  const int head = kvh * p.group + in_slot - token * p.group;
-  uint8_t* out = p.out.data + 2 * ((int64_t)b * p.out.batch_stride + (int64_t)t * p.out.token_stride + (int64_t)head * p.out.head_stride + col4 * 4);
-  *reinterpret_cast<uint2*>(out) = make_uint2(cache::pack_bf16(o[0] * inv, o[1] * inv), cache::pack_bf16(o[2] * inv, o[3] * inv));
-  if (p.lse && col4 == 0) p.lse[((int64_t)b * p.n + t) * p.heads + head] = l == 0.f ? -INFINITY : kLn2 * (r + log2f(l));
 }
 
 }  // namespace attn

@@ -156,10 +156,13 @@ cudaError_t launch(fly_attention* h, const CUtensorMap* maps, const A::Params& p
   cudaError_t e = cudaLaunchKernelEx(&cfg, A::attention_kernel<D, E4M3, PAIR>, maps[0], maps[1], maps[2], p);
   if (e != cudaSuccess || h->sm_count < 2) return e;
   h->last_launches++;
-  fill_launch(&cfg, attr, (unsigned)h->sm_count - 1, D * 8, st, true);
-  const int used = PAIR ? S::kItemRows : p.tpt * p.group;
-  cfg.gridDim.y = (unsigned)((used + 31) / 32);
-  e = cudaLaunchKernelEx(&cfg, A::attention_combine_kernel<D, S::kItemRows>, p);
+  // Nothing is cut where every item is short enough to stay whole, whatever the lengths are.
+  if (p.groups <= 32 && (int64_t)p.groups * p.c.kv_heads <= h->sm_count && p.c.capacity <= A::kWholeItem * A::kTile) return e;
+  // (blocks for as many cut items as there can be, at most four per SM)
+  const int64_t items = (int64_t)p.groups * p.c.kv_heads, most = (items < h->sm_count - 1 ? items : h->sm_count - 1) * (PAIR ? S::kItemRows : p.tpt * p.group) * (D / 4);
+  const int64_t blocks = (most + A::kCombineThreads - 1) / A::kCombineThreads;
+  fill_launch(&cfg, attr, (unsigned)(blocks < 4 * h->sm_count ? blocks : 4 * h->sm_count), A::kCombineThreads, st, true);
+  e = cudaLaunchKernelEx(&cfg, A::attention_combine_kernel<D, S::kItemRows>, p, h->sm_count);
   if (e == cudaSuccess) h->last_launches++;
   return e;
 }
