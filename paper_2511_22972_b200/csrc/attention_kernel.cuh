@@ -241,7 +241,7 @@ struct Shape {
   static constexpr int kOffV = kOffK + kKStages * kKBytes;
   static constexpr int kOffRaw = kOffV + kVStages * kTileBytes;
   static constexpr int kOffScales = kOffRaw + kRawStages * kRawBytes;
-  static constexpr int kOffExchange = kOffScales + (E4M3 ? (kScaleRing + 1) * kTile * 4 + kKStages * kTile : 0);  // fp32, ones, bytes by stage
+  static constexpr int kOffExchange = kOffScales + (E4M3 ? kScaleRing * kTile * 4 + kKStages * kTile : 0);  // fp32, bytes by stage
   static constexpr int kOffBar = kOffExchange + 2 * kTileRows * 8;
   static constexpr int kNumBars = 3 * kKStages + 2 * kVStages + 2 * kRawStages + 4 + 6;
   static constexpr int kOffFlags = kOffBar + kNumBars * 8;
@@ -443,23 +443,6 @@ __device__ __forceinline__ void scale32(uint32_t (&r)[32], const float* scales) 
     r[c + 3] = __float_as_uint(y);
   }
 }
-// Scores that a row does not see become -inf, in tensor memory, for tiles where there are any (E4M3: after the keys' scales, which may be NaN).  32
-// columns at a time in a loop: code that runs once an item is fetched anew each time, about four cycles an instruction, and as part
-// of the unrolled step below the mask took 4000 cycles.
-template <bool E4M3>
-__device__ __forceinline__ void hide(uint32_t ts, const RowMask& mask, const float* scales) {
-  uint32_t r[32];
-#pragma unroll 1
-  for (int c0 = 0; c0 < kTile; c0 += 32) {
-    tmem_ld32(ts + c0, r);
-    if (E4M3) scale32(r, scales + c0);
-    const uint32_t v = mask.bits(c0);
-#pragma unroll
-    for (int c = 0; c < 32; ++c) r[c] = v & (1u << c) ? r[c] : 0xff800000u;
-    tmem_st32(ts + c0, r);
-  }
-  tmem_st_wait();
-}
 __device__ __forceinline__ float max32(const uint32_t (&r)[32], float mx) {
   float m[4];
 #pragma unroll
@@ -488,72 +471,90 @@ __device__ __forceinline__ void exp32(const uint32_t (&r)[32], f2 sc2, f2 nr2, f
 
 constexpr int kOffP = 64;  // P's first column over S: its columns are taken from the last to the first
 
+// The row's reference moves where its maximum has passed it by 8 binades: sum and O follow.
+template <int D>
+__device__ __forceinline__ void move_reference(uint32_t to, float top, bool first, float& ref, float& sum) {
+  const bool move = top > ref + 8.0f;  // (false for a row that has seen nothing, and for NaN)
+  if (!__any_sync(0xffffffffu, move)) return;
+  const float alpha = move ? (ref == -INFINITY ? 0.f : ex2_approx(ref - top)) : 1.f;
+  if (move) ref = top;
+  sum *= alpha;
+  if (first) return;
+  uint32_t a[32];
+#pragma unroll 1
+  for (int h = 0; h < D / 32; ++h) {
+    tmem_ld32(to + h * 32, a);
+#pragma unroll
+    for (int c = 0; c < 32; ++c) a[c] = __float_as_uint(__uint_as_float(a[c]) * alpha);
+    tmem_st32(to + h * 32, a);
+  }
+}
+
 // One step of a row: S in tensor memory at `ts` becomes P there, the row's reference and sum move on, and O at `to` is rescaled if it must be.
 // Columns come 32 at a time, the next ones on their way while one block is worked on; the last block of the maximum is the
-// first of the exponentials.  E4M3: one block after the other, in loops: there are more warps with code of their own, and short loops spare
-// the instruction caches (16 sequences of nine over e4m3 189 -> 158 us; bf16 chunks of 2000 1003 -> 1045, so not there).
-template <int D, bool E4M3>
-__device__ __forceinline__ void softmax_step(uint32_t ts, uint32_t to, float scale, bool first, const float* scales, float& ref, float& sum) {
+// first of the exponentials.
+template <int D>
+__device__ __forceinline__ void softmax_step(uint32_t ts, uint32_t to, float scale, bool first, float& ref, float& sum) {
   uint32_t a[32], b[32];
-  float mx = -INFINITY;
-  if (E4M3) {
-#pragma unroll 1
-    for (int h = 0; h < 4; ++h) {
-      tmem_ld32(ts + h * 32, b);
-      scale32(b, scales + h * 32);
-      mx = max32(b, mx);
-    }
-  } else {
-    tmem_ld32(ts, a);
-    tmem_ask32(ts + 32, b);
-    mx = max32(a, mx);
-    tmem_wait(b);
-    tmem_ask32(ts + 64, a);
-    mx = max32(b, mx);
-    tmem_wait(a);
-    tmem_ask32(ts + 96, b);
-    mx = max32(a, mx);
-    tmem_wait(b);
-    mx = max32(b, mx);
-  }
-  const float top = mx * scale;
-  const bool move = top > ref + 8.0f;  // (false for a row that has seen nothing, and for NaN)
-  if (__any_sync(0xffffffffu, move)) {
-    const float alpha = move ? (ref == -INFINITY ? 0.f : ex2_approx(ref - top)) : 1.f;
-    if (move) ref = top;
-    sum *= alpha;
-    if (!first) {
-#pragma unroll 1
-      for (int h = 0; h < D / 32; ++h) {
-        tmem_ld32(to + h * 32, a);
-#pragma unroll
-        for (int c = 0; c < 32; ++c) a[c] = __float_as_uint(__uint_as_float(a[c]) * alpha);
-        tmem_st32(to + h * 32, a);
-      }
-    }
-  }
+  tmem_ld32(ts, a);
+  tmem_ask32(ts + 32, b);
+  float mx = max32(a, -INFINITY);
+  tmem_wait(b);
+  tmem_ask32(ts + 64, a);
+  mx = max32(b, mx);
+  tmem_wait(a);
+  tmem_ask32(ts + 96, b);
+  mx = max32(a, mx);
+  tmem_wait(b);
+  mx = max32(b, mx);
+  move_reference<D>(to, mx * scale, first, ref, sum);
   const float nr = ref == -INFINITY ? 0.f : -ref;
   const f2 sc2 = pack2(scale, scale), nr2 = pack2(nr, nr);
   f2 acc[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
-  if (E4M3) {
 #pragma unroll 1
-    for (int h = 3; h >= 0; --h) {
-      if (h < 3) {
-        tmem_ld32(ts + h * 32, b);
-        scale32(b, scales + h * 32);
-      }
-      exp32(b, sc2, nr2, acc, ts + kOffP + h * 16);
-    }
-  } else {
+  for (int h = 1; h >= 0; --h) {
+    tmem_ask32(ts + h * 64, a);
+    exp32(b, sc2, nr2, acc, ts + kOffP + h * 32 + 16);
+    tmem_wait(a);
+    if (h != 0) tmem_ask32(ts + 32, b);
+    exp32(a, sc2, nr2, acc, ts + kOffP + h * 32);
+    if (h != 0) tmem_wait(b);
+  }
+  float x, y;
+  unpack2(add2(acc[0], acc[1]), x, y);
+  sum += x + y;
+}
+
+// The same in short loops over blocks b0 .. b1 - 1 of 32 columns: for tiles in which some row does not see every position (scores that it does not see
+// become -inf, after the keys' scales, which may be NaN there; blocks that no row sees are left out), and for all tiles of codes, where
+// more warps have code of their own: what is not in a short loop is fetched anew each time, about four cycles an instruction (16
+// sequences of nine over e4m3 189 -> 158 us; bf16 chunks of 2000 1003 -> 1045, so not there).
+template <int D, bool E4M3>
+__device__ __forceinline__ void softmax_blocks(uint32_t ts, uint32_t to, float scale, bool first, bool masked, const RowMask& mask, int b0, int b1,
+                                               const float* scales, float& ref, float& sum) {
+  uint32_t a[32];
+  float mx = -INFINITY;
 #pragma unroll 1
-    for (int h = 1; h >= 0; --h) {
-      tmem_ask32(ts + h * 64, a);
-      exp32(b, sc2, nr2, acc, ts + kOffP + h * 32 + 16);
-      tmem_wait(a);
-      if (h != 0) tmem_ask32(ts + 32, b);
-      exp32(a, sc2, nr2, acc, ts + kOffP + h * 32);
-      if (h != 0) tmem_wait(b);
+  for (int h = b0; h < b1; ++h) {
+    tmem_ld32(ts + h * 32, a);
+    if (E4M3) scale32(a, scales + h * 32);
+    if (masked) {
+      const uint32_t v = mask.bits(h * 32);
+#pragma unroll
+      for (int c = 0; c < 32; ++c) a[c] = v & (1u << c) ? a[c] : 0xff800000u;
     }
+    if (masked || E4M3) tmem_st32(ts + h * 32, a);
+    mx = max32(a, mx);
+  }
+  if (masked || E4M3) tmem_st_wait();
+  move_reference<D>(to, mx * scale, first, ref, sum);
+  const float nr = ref == -INFINITY ? 0.f : -ref;
+  const f2 sc2 = pack2(scale, scale), nr2 = pack2(nr, nr);
+  f2 acc[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+#pragma unroll 1
+  for (int h = b1 - 1; h >= b0; --h) {
+    tmem_ld32(ts + h * 32, a);
+    exp32(a, sc2, nr2, acc, ts + kOffP + h * 16);
   }
   float x, y;
   unpack2(add2(acc[0], acc[1]), x, y);
@@ -623,7 +624,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
   volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(smem + S::kOffMisc);  // [0] tensor memory, [1] a role gave up, [8..15] items with values to add back
   volatile uint32_t* tile_bad = reinterpret_cast<volatile uint32_t*>(smem + S::kOffFlags);  // of tile number t: entry t % 16, for the conversion 16 + t % 16
   float* key_scales = reinterpret_cast<float*>(smem + S::kOffScales);  // of tile number t: entry t % kScaleRing
-  uint8_t* key_bytes = smem + S::kOffScales + (S::kScaleRing + 1) * kTile * 4;
+  uint8_t* key_bytes = smem + S::kOffScales + S::kScaleRing * kTile * 4;
   float2* exchange = reinterpret_cast<float2*>(smem + S::kOffExchange);
 
   const int tid = (int)threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -646,8 +647,6 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       mbar_init(o_full(s), 1);
     }
     misc[1] = 0;
-    if (E4M3)
-      for (int i = 0; i < kTile; ++i) key_scales[S::kScaleRing * kTile + i] = 1.f;
     for (int i = 8; i < 16; ++i) misc[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -1069,16 +1068,18 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         const uint32_t bad = tile_bad[(tile_no + (uint32_t)j) & 15];
         if (warp_live) {
           tc_fence_after();
-          if (p0 + kTile > first_hi || (p0 < last_lo && p0 + kTile > p.sinks) || bad != 0) {
+          const bool masked = p0 + kTile > first_hi || (p0 < last_lo && p0 + kTile > p.sinks) || bad != 0;
+          if (masked || E4M3) {
             RowMask mask;
             mask.bad = bad;
             mask.lim = min(row_pos + 1, g.hi) - p0;
             mask.lo = p.window > 0 ? row_pos + 1 - p.window - p0 : 0;
             mask.snk = p.sinks - p0;
-            hide<E4M3>(ts, mask, key_scales + ((tile_no + (uint32_t)j) % S::kScaleRing) * kTile);
-            softmax_step<D, E4M3>(ts, to, scale, !begun, key_scales + S::kScaleRing * kTile, ref, sum);
+            const Span span = tile_span(p, g, p0);
+            softmax_blocks<D, E4M3>(ts, to, scale, !begun, masked, mask, span.first / 32, (span.last + 31) / 32, key_scales + ((tile_no + (uint32_t)j) % S::kScaleRing) * kTile, ref,
+                                    sum);
           } else {
-            softmax_step<D, E4M3>(ts, to, scale, !begun, key_scales + ((tile_no + (uint32_t)j) % S::kScaleRing) * kTile, ref, sum);
+            softmax_step<D>(ts, to, scale, !begun, ref, sum);
           }
           tmem_st_wait();
           tc_fence_before();
