@@ -637,13 +637,13 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       mbar_init(k_empty(s), 1);
       if (E4M3) mbar_init(k_ready(s), 1);
     }
-    for (int s = 0; s < S::kVStages; ++s) { mbar_init(v_full(s), E4M3 ? S::kConvThreads : 1); mbar_init(v_empty(s), 1); }
-    for (int s = 0; s < S::kRawStages; ++s) { mbar_init(raw_full(s), 33); mbar_init(raw_empty(s), S::kConvThreads); }
+    for (int s = 0; s < S::kVStages; ++s) { mbar_init(v_full(s), E4M3 ? S::kConvWarps : 1); mbar_init(v_empty(s), 1); }
+    for (int s = 0; s < S::kRawStages; ++s) { mbar_init(raw_full(s), 33); mbar_init(raw_empty(s), S::kConvWarps); }
     for (int s = 0; s < 2; ++s) {
       mbar_init(q_full(s), E4M3 ? (PAIR ? kTileRows : 2 * kTileRows) : 1);
       mbar_init(q_empty(s), 1);
       mbar_init(s_full(s), 1);
-      mbar_init(p_ready(s), kTileRows);
+      mbar_init(p_ready(s), kTileRows / 32);
       mbar_init(o_full(s), 1);
     }
     misc[1] = 0;
@@ -990,7 +990,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         }
         if (any) misc[8 + (item & 7)] = item + 1;
         async_proxy_fence();
-        if (!failed) {
+        __syncwarp();
+        if (!failed && lane == 0) {
           mbar_arrive(v_full(st));
           mbar_arrive(raw_empty(rs));
         }
@@ -1120,7 +1121,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
           __syncwarp();
         }
         begun = true;
-        mbar_arrive(p_ready(slot));
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_ready(slot));
       }
       // ---- the item's end ----
       if (begun) {

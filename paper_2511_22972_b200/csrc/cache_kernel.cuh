@@ -128,8 +128,8 @@ __device__ __forceinline__ void plain16_e4m3(const uint4& codes, int s, uint32_t
   for (int i = 0; i < 4; ++i) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const uint32_t h = __byte_perm(c[i], 0u, k ? 0x3424 : 0x1404);  // two codes in the upper bytes
-      const uint32_t v = (h & 0x80008000u) | ((h >> 4) & 0x07f007f0u);
+      const uint32_t h = __byte_perm(c[i], 0u, k ? 0x4342 : 0x4140);  // two codes in the lower bytes
+      const uint32_t v = (h & 0x00800080u) * 0xf0u + h * 16u;        // four places up, the sign (2^7, now 2^11) to 2^15: two of the four on the FMA pipe
       asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(w[2 * i + k]) : "r"(v), "r"(f));
     }
   }
