@@ -90,9 +90,9 @@ __device__ __forceinline__ Group group_at(const Params& p, int g) {
   r.lo_first = lo;
   r.lo_last = p.window > 0 ? max(0, r.L + r.t1 - p.window) : 0;
   const int nt = (r.hi + kTile - 1) / kTile;
-  r.lo_tile = lo / kTile;
+  r.lo_tile = lo < r.hi ? lo / kTile : nt;  // (a window behind the table's end has no tile)
   r.ns = min(min(r.lo_tile, nt), (min(p.sinks, lo) + kTile - 1) / kTile);
-  r.count = r.ns + max(0, nt - r.lo_tile);
+  r.count = r.ns + nt - r.lo_tile;
   return r;
 }
 __device__ __forceinline__ int tile_start(const Group& g, int x) { return (x < g.ns ? x : g.lo_tile + x - g.ns) * kTile; }
@@ -243,7 +243,7 @@ struct Shape {
   static constexpr int kOffScales = kOffRaw + kRawStages * kRawBytes;
   static constexpr int kOffExchange = kOffScales + (E4M3 ? kScaleRing * kTile * 4 + kKStages * kTile : 0);  // fp32, bytes by stage
   static constexpr int kOffBar = kOffExchange + 2 * kTileRows * 8;
-  static constexpr int kNumBars = 3 * kKStages + 2 * kVStages + 2 * kRawStages + 4 + 6;
+  static constexpr int kNumBars = 3 * kKStages + 2 * kVStages + 2 * kRawStages + 4 + 6 + 1;
   static constexpr int kOffFlags = kOffBar + kNumBars * 8;
   static constexpr int kOffMisc = kOffFlags + 2 * 16 * 4;
   static constexpr int kSmem = kOffMisc + 64;
@@ -299,7 +299,7 @@ __device__ __forceinline__ Range range_of(const Params& p) {  // (the host has s
   const int first = (int)begin;
   r.tiles = min(r.share, sum - first);
   int run = 0;
-  for (int base = 0;; base += 32) {
+  for (int base = 0; base < p.groups; base += 32) {
     if (base > 0) g0 = group_at(p, min(base + lane, p.groups - 1));
     const int v = base == 0 ? (r.item_cost < 0 ? min(count0, p.c.kv_heads) : count0) : base + lane < p.groups ? work_of(p, g0) : 0;
     int x = x0;
@@ -330,6 +330,8 @@ __device__ __forceinline__ Range range_of(const Params& p) {  // (the host has s
     }
     run += __shfl_sync(0xffffffffu, x, 31);
   }
+  r.tiles = 0;  // (lengths that change while they are read)
+  return r;
 }
 
 // A role's walk over the items of its CTA's range: tiles x0 .. x1 - 1 of item (g, kvh).
@@ -378,6 +380,12 @@ __device__ __forceinline__ bool slot_sees(const Params& p, const Group& g, int s
   const int ts0 = g.t0 + s * p.tpt, ts1 = min(g.t1, ts0 + p.tpt);
   if (ts0 >= ts1 || p0 >= g.L + ts1) return false;
   return p.window == 0 || p0 + kTile - 1 > g.L + ts0 - p.window || p0 < p.sinks;
+}
+// The last of the tiles x0 .. x0 + m - 1 of which slot s of a pair sees anything, counted from x0; -1: none.
+__device__ __forceinline__ int last_seen(const Params& p, const Group& g, int s, int x0, int m) {
+  int j = g.t0 + s * p.tpt < g.t1 ? m - 1 : -1;
+  while (j >= 0 && !slot_sees(p, g, s, tile_start(g, x0 + j))) --j;  // (a few tiles from the end)
+  return j;
 }
 // 0: no row of the item sees position pos, 1: some do, 2: all.
 __device__ __forceinline__ int seen_by(const Params& p, const Group& g, int pos) {
@@ -616,6 +624,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
   auto raw_empty = [&](uint32_t s) { return bar0 + 8u * (2 * S::kKStages + 2 * S::kVStages + S::kRawStages + s); };
   constexpr uint32_t kB = 2 * S::kKStages + 2 * S::kVStages + 2 * S::kRawStages, kRaw = E4M3 ? S::kRawStages : 1;
   auto k_ready = [&](uint32_t s) { return E4M3 ? bar0 + 8u * (kB + 10 + s) : k_full(s); };  // ... and for E4M3 its keys' scales are in fp32
+  const uint32_t drained = bar0 + 8u * (S::kNumBars - 1);                  // (after a wait has run out) no MMA is in flight
   auto q_full = [&](int s) { return bar0 + 8u * (kB + s); };
   auto q_empty = [&](int s) { return bar0 + 8u * (kB + 2 + s); };
   auto s_full = [&](int s) { return bar0 + 8u * (kB + 4 + s); };          // S of a slot's step is complete (and every MMA before it)
@@ -646,6 +655,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       mbar_init(p_ready(s), kTileRows / 32);
       mbar_init(o_full(s), 1);
     }
+    mbar_init(drained, 1);
     misc[1] = 0;
     for (int i = 8; i < 16; ++i) misc[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -669,13 +679,10 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
   asm volatile("griddepcontrol.wait;" ::: "memory");  // everything below reads or writes what the kernels before may be working on
   asm volatile("griddepcontrol.launch_dependents;");
 
-  // A wait has run out, or had in a step before and nobody has looked: no wait waits any more, and nothing is issued.  (One lane looks: a warp's
-  // lanes decide alike.)
-  bool failed = __shfl_sync(0xffffffffu, lane == 0 ? *reinterpret_cast<volatile int*>(p.status) : 0, 0) != 0;
-  auto wait = [&](uint32_t bar, uint32_t parity) {
-    if (!failed && !mbar_wait_suspended(bar, parity, p.status, kErrAttention)) failed = true;
-    __syncwarp();
-  };
+  // A wait has run out, or had in a step before and nobody has looked: no wait waits any more, nothing is issued, and nothing that others
+  // write is read: all that is left to do is NaN for the rows.  (One lane looks: a warp's lanes decide alike.)
+  const bool pending = __shfl_sync(0xffffffffu, lane == 0 ? *reinterpret_cast<volatile int*>(p.status) : 0, 0) != 0;
+  bool failed = pending;
   auto wait_warp = [&](uint32_t bar, uint32_t parity) {  // the same decision in the whole warp
     if (!failed && !__all_sync(0xffffffffu, mbar_wait_suspended(bar, parity, p.status, kErrAttention))) failed = true;
   };
@@ -770,11 +777,12 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         for (int j = 0; j < m; ++j) {
           const uint32_t no = tile_no + (uint32_t)j, st = no % S::kKStages;
           wait_warp(k_full(st), (no / S::kKStages) & 1);
+          if (failed) break;
           const uint32_t b = *reinterpret_cast<const uint32_t*>(key_bytes + st * kTile + 4 * lane);
           *reinterpret_cast<float4*>(key_scales + (no % S::kScaleRing) * kTile + 4 * lane) =
               make_float4(cache::scale_value(b & 255u), cache::scale_value((b >> 8) & 255u), cache::scale_value((b >> 16) & 255u), cache::scale_value(b >> 24));
           __syncwarp();
-          if (!failed && lane == 0) mbar_arrive(k_ready(st));
+          if (lane == 0) mbar_arrive(k_ready(st));
           __syncwarp();
         }
         tile_no += m;
@@ -812,7 +820,9 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     __syncwarp();
     const bool lead = elect_lane();
     constexpr uint32_t kIdescS = instr_desc(kTile, false), kIdescO = instr_desc(D, true);
-    uint32_t item = 0, use0 = 0, use1 = 0;  // steps of each slot so far
+    uint32_t item = 0, use0 = 0, use1 = 0;   // steps of each slot so far
+    uint32_t queries0 = 0, queries1 = 0;     // items of which a slot of a pair has had its queries
+    bool issued = false;
     for (; walk.have(); walk.next(), ++item) {
       const Group& g = walk.gr;
       const int m = walk.tiles();
@@ -820,6 +830,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       auto issue_s = [&](int s, int j) {  // S of slot s = Q x keys of tile j
         const uint32_t st = (tile_no + (uint32_t)j) % S::kKStages;
         const int buf = PAIR ? s : (int)(item % S::kQBufs);
+        issued |= !failed;
         if (!failed && lead) {
           const uint32_t a = desc_lo(base + buf * S::kTileBytes, 16), b = desc_lo(base + S::kOffK + st * S::kKBytes, 16);
           if (E4M3) {
@@ -875,12 +886,13 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       auto release_k = [&](int j) { commit(k_empty((tile_no + (uint32_t)j) % S::kKStages)); };
       auto release_v = [&](int j) { commit(v_empty((tile_no + (uint32_t)j) % S::kVStages)); };
       if (PAIR) {
-        wait_warp(q_full(0), item & 1);
-        wait_warp(q_full(1), item & 1);
-        int last[2] = {-1, -1};
-        for (int s = 0; s < 2; ++s)  // (a few tiles from the end, unless the slot has no token)
-          if (g.t0 + s * p.tpt < g.t1)
-            for (last[s] = m - 1; last[s] >= 0 && !sees(s, last[s]); --last[s]) {}
+        int last[2];
+        for (int s = 0; s < 2; ++s) {
+          last[s] = last_seen(p, g, s, walk.x0, m);
+          if (E4M3 && last[s] < 0) continue;  // (then its warps bring no queries)
+          wait_warp(q_full(s), (s ? queries1 : queries0) & 1);
+          ++(s ? queries1 : queries0);
+        }
         bool begun[2] = {false, false};
         wait_k(0);
         for (int s = 0; s < 2; ++s)
@@ -927,10 +939,9 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       }
       tile_no += m;
     }
-    if (failed && lead) {  // what has been issued ends before shared and tensor memory are given back
-      mma_commit(q_full(0));
-      const unsigned long long t0 = global_ns();
-      while (global_ns() - t0 < 2000000ull) {}
+    if (failed && issued) {  // what has been issued ends before shared and tensor memory are given back
+      if (lead) mma_commit(drained);
+      mbar_wait_quiet(drained, 0, 2000000ull);
     }
     __syncwarp();
   }
@@ -951,6 +962,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         const uint32_t no = tile_no + (uint32_t)j, rs = no % kRaw, st = no % S::kVStages;
         wait_warp(raw_full(rs), (no / kRaw) & 1);
         wait_warp(v_empty(st), ((no / S::kVStages) & 1) ^ 1);
+        if (failed) break;
         const uint8_t* raw = smem + S::kOffRaw + rs * S::kRawBytes;
         uint8_t* dst = smem + S::kOffV + st * S::kTileBytes;
         const int p0 = tile_start(g, walk.x0 + j);
@@ -991,12 +1003,13 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         if (any) misc[8 + (item & 7)] = item + 1;
         async_proxy_fence();
         __syncwarp();
-        if (!failed && lane == 0) {
+        if (lane == 0) {
           mbar_arrive(v_full(st));
           mbar_arrive(raw_empty(rs));
         }
         __syncwarp();
       }
+      if (failed) break;
       tile_no += m;
     }
   } else {
@@ -1016,12 +1029,12 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       const int first_hi = min(g.L + ts0 + 1, g.hi), last_lo = p.window > 0 ? g.L + ts1 - p.window : 0;
       float ref = -INFINITY, sum = 0.f, scale = p.scale;
       bool begun = false;
-      if (E4M3) {
+      if (E4M3 && (!PAIR || last_seen(p, g, slot, walk.x0, m) >= 0)) {
         // The row's queries in two parts (of one row tile: both slots take half of the columns).  Every MMA that read the item before's is done: its O was
-        // waited for.
+        // waited for.  A slot that sees nothing brings none: it waits for nothing either, and would run on past the phase that the MMAs wait for.
         constexpr int kPieces = PAIR ? D / 8 : D / 16;  // of eight values
         const int piece0 = PAIR ? 0 : slot * kPieces;
-        const bool there = row_token < p.tpt && t < p.n;
+        const bool there = !failed && row_token < p.tpt && t < p.n;
         const uint4* from = reinterpret_cast<const uint4*>(p.q.data + 2 * ((int64_t)g.b * p.q.batch_stride + (int64_t)t * p.q.token_stride +
                                                                            (int64_t)(walk.kvh * p.group + row_head) * p.q.head_stride)) + piece0;
         uint32_t m2 = 0u;
@@ -1053,18 +1066,20 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
 #pragma unroll
             for (int c = 0; c < 8; c += 2) cache::split_e4m3_e5m2(x[c], x[c + 1], inv, w[c / 2], w[4 + c / 2]);
           }
+          if (failed) continue;
           const int at = code_at(D, row, (piece0 + i) / 2);
           *reinterpret_cast<uint4*>(hi + at) = make_uint4(w[0], w[1], w[2], w[3]);
           *reinterpret_cast<uint4*>(hi + S::kCodeBytes + at) = make_uint4(w[4], w[5], w[6], w[7]);
         }
         async_proxy_fence();
-        mbar_arrive(q_full(PAIR ? slot : 0));
+        if (!failed) mbar_arrive(q_full(PAIR ? slot : 0));
         if (!PAIR) asm volatile("bar.sync 1, 256;" ::: "memory");  // (the exchange is used again at the item's end)
       }
       for (int j = PAIR ? 0 : slot; j < m; j += PAIR ? 1 : 2) {
         const int p0 = tile_start(g, walk.x0 + j);
         if (PAIR && !slot_sees(p, g, slot, p0)) continue;
-        wait(s_full(slot), use & 1);
+        wait_warp(s_full(slot), use & 1);
+        if (failed) break;
         ++use;
         const uint32_t bad = tile_bad[(tile_no + (uint32_t)j) & 15];
         if (warp_live) {
@@ -1088,7 +1103,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         if (!E4M3 && (bad != 0 || tile_unseen(p, g, p0) || tile_partial(p, g, p0)) && (!PAIR || slot == 0 || !slot_sees(p, g, 0, p0))) {
           // The values' tile before its MMAs (those of both slots come after this slot's p_ready), 16 bytes at a time: only what the MMAs take.
           const uint32_t no = tile_no + (uint32_t)j, st = no % S::kVStages;
-          wait(v_full(st), (no / S::kVStages) & 1);
+          wait_warp(v_full(st), (no / S::kVStages) & 1);
+          if (failed) break;
           uint8_t* tile = smem + S::kOffV + st * S::kTileBytes;
           const Span span = tile_span(p, g, p0);
           bool any = false;
@@ -1125,16 +1141,16 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         if (lane == 0) mbar_arrive(p_ready(slot));
       }
       // ---- the item's end ----
-      if (begun) {
-        wait(o_full(slot), items_done & 1);
+      if (begun && !failed) {
+        wait_warp(o_full(slot), items_done & 1);
         ++items_done;
         tc_fence_after();
       }
       const bool from_start = walk.x0 == 0, whole = from_start && walk.x1 == g.count;
       float w0 = 1.f, w1 = 0.f, r = ref, l = sum;
-      bool use0 = PAIR ? begun : true, use1 = false;
+      bool use0 = PAIR ? begun : true, use1 = false;  // whether there is an O of each slot
       if (!PAIR) {
-        exchange[slot * kTileRows + row] = make_float2(ref, sum);
+        exchange[slot * kTileRows + row] = make_float2(ref, failed ? __uint_as_float(0x7fc00000u) : sum);  // (the other slot's columns are NaN too)
         asm volatile("bar.sync 1, 256;" ::: "memory");  // both slots' O are complete as well
         const float2 a = exchange[row], b = exchange[kTileRows + row];
         use1 = m > 1;
@@ -1145,7 +1161,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         l = a.y * w0 + (use1 ? b.y * w1 : 0.f);
         tc_fence_after();
       }
-      const bool poison = misc[8 + (item & 7)] == item + 1;  // (read when both slots are done where they share the item)
+      if (failed) use0 = use1 = false;
+      const bool poison = !failed && misc[8 + (item & 7)] == item + 1;  // (read when both slots are done where they share the item)
       if (warp_live) {
         const float inv = failed ? __uint_as_float(0x7fc00000u) : whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
         const int head = walk.kvh * p.group + row_head;
@@ -1170,7 +1187,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             for (int c = 0; c < 16; ++c) o[c] = z[c];
           }
 #pragma unroll
-          for (int c = 0; c < 16; ++c) o[c] *= inv;
+          for (int c = 0; c < 16; ++c) o[c] *= inv;  // (NaN if a wait has run out)
           if (live) {
             if (whole) {
 #pragma unroll
@@ -1198,7 +1215,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     }
   }
 
-  if (failed) misc[1] = 1;
+  if (failed && !pending) misc[1] = 1;
   tc_fence_before();
   __syncthreads();
   if (misc[1] != 0) {  // stragglers among the loads

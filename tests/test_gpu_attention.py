@@ -272,3 +272,47 @@ def test_refusals():
         assert e.value.status == Bd.FLY_ERR_UNSUPPORTED
     with pytest.raises(Bd.FlyError):
         ChunkAttention(2, 4, 8, 4, 64).run(pool.cache, q, torch.zeros_like(q), **ok)   # another shape than the cache's
+
+
+# ---- row tiles without work, windows behind the table's end, waits that run out in every form of the kernel ------------------
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (43, 20)])
+def test_pairs_of_row_tiles_of_which_one_is_empty(fmt, window, sinks):
+    # two heads to a key/value head: 64 tokens to a row tile.  Many chunks end in the first tile of a pair, eight heads one after the other,
+    # several items to an SM.
+    n, lengths = 130, [5 * b for b in range(40)]
+    counts = [(30, 130, 64, 129, 1)[b % 5] for b in range(40)]
+    pool = held(lengths, n, 8, 64, 128, fmt, seed=6)
+    att = ChunkAttention(40, n, 16, 8, 64)
+    for _ in range(3):
+        run(pool, n, 16, window, sinks, counts=counts, handle=att, rows_of={0, 63, 64, 128, 129})
+    assert att.device_status(stream()) == Bd.FLY_OK
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("n", [12, 70])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (5, 0), (5, 3), (5, 300), (300, 40)])
+def test_windows_that_end_behind_the_table(fmt, n, window, sinks):
+    # what is behind the table does not exist: later rows see less and less of the window, then the first tokens only, or nothing
+    full = Pool([304, 304, 304, 304], 0, 2, 64, 16, fmt, seed=n)
+    full.lengths = torch.tensor([304, 300, 250, 304 - n], dtype=torch.int32)
+    full.refresh()
+    run(full, n, 16, window, sinks, rows_of=set(range(0, n, 5)) | {n - 1})
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("n", [3, 40])
+def test_every_form_gives_nan_while_a_wait_that_ran_out_is_pending(fmt, dim, n):
+    pool = held([700, 20], n, 2, dim, 16, fmt, seed=3)
+    att = ChunkAttention(2, n, 16, 2, dim)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q = rows(2, n, 16, dim, g)
+    out, lse = torch.zeros_like(q), torch.zeros(2, n, 16, device="cuda")
+    assert att.selftest_wait(stream()) == Bd.FLY_OK
+    for _ in range(2):
+        att.run(pool.cache, q, out, lse=lse, stream=stream())
+    assert att.device_status(stream()) == Bd.FLY_ERR_TIMEOUT
+    assert bool(out.isnan().all()) and bool(lse.isnan().all())
+    run(pool, n, 16, handle=att, rows_of={0, n - 1})
