@@ -47,6 +47,7 @@ namespace attn {
 constexpr int kTile = 128;      // positions per step
 constexpr int kTileRows = 128;  // rows per slot
 constexpr int kErrAttention = 5;
+__device__ __forceinline__ float quiet_nan() { return __uint_as_float(0x7fc00000u); }
 
 struct Params {
   cache::View c;
@@ -601,6 +602,13 @@ __device__ __noinline__ void add_back(const Params& p, int b, int kvh, int row_p
   visit(upper, hi);                      // ... and that only later ones do
 }
 
+// A row's result where a wait has run out.
+__device__ __noinline__ void nan_row(const Params& p, int b, int t, int head, int D) {
+  uint4* o = reinterpret_cast<uint4*>(p.out.data + 2 * ((int64_t)b * p.out.batch_stride + (int64_t)t * p.out.token_stride + (int64_t)head * p.out.head_stride));
+  for (int i = 0; i < D / 8; ++i) o[i] = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
+  if (p.lse) p.lse[((int64_t)b * p.n + t) * p.heads + head] = quiet_nan();
+}
+
 // Where a part of an item lies in scratch, in units of four columns of a row: neighbouring rows side by side, so that a warp's stores and
 // loads are whole lines (a row after the other they took 4 - 9 thousand cycles of an item's end).
 template <int D, int ROWS>
@@ -1141,7 +1149,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         if (lane == 0) mbar_arrive(p_ready(slot));
       }
       // ---- the item's end ----
-      if (begun && !failed) {
+      if (begun) {
         wait_warp(o_full(slot), items_done & 1);
         ++items_done;
         tc_fence_after();
@@ -1150,7 +1158,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       float w0 = 1.f, w1 = 0.f, r = ref, l = sum;
       bool use0 = PAIR ? begun : true, use1 = false;  // whether there is an O of each slot
       if (!PAIR) {
-        exchange[slot * kTileRows + row] = make_float2(ref, failed ? __uint_as_float(0x7fc00000u) : sum);  // (the other slot's columns are NaN too)
+        exchange[slot * kTileRows + row] = make_float2(ref, failed ? quiet_nan() : sum);  // (the other slot's columns are NaN too)
         asm volatile("bar.sync 1, 256;" ::: "memory");  // both slots' O are complete as well
         const float2 a = exchange[row], b = exchange[kTileRows + row];
         use1 = m > 1;
@@ -1161,11 +1169,15 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         l = a.y * w0 + (use1 ? b.y * w1 : 0.f);
         tc_fence_after();
       }
-      if (failed) use0 = use1 = false;
-      const bool poison = !failed && misc[8 + (item & 7)] == item + 1;  // (read when both slots are done where they share the item)
-      if (warp_live) {
-        const float inv = failed ? __uint_as_float(0x7fc00000u) : whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-        const int head = walk.kvh * p.group + row_head;
+      const bool poison = misc[8 + (item & 7)] == item + 1;  // (read when both slots are done where they share the item)
+      const int head = walk.kvh * p.group + row_head;
+      if (failed) {
+        if (live) {
+          if (whole) nan_row(p, g.b, t, head, D);
+          else p.part_ml[((int64_t)blockIdx.x * 2 + (from_start ? 1 : 0)) * S::kItemRows + (PAIR ? slot * kTileRows : 0) + row] = make_float2(0.f, quiet_nan());
+        }
+      } else if (warp_live) {
+        const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
         uint8_t* out = p.out.data + 2 * ((int64_t)g.b * p.out.batch_stride + (int64_t)t * p.out.token_stride + (int64_t)head * p.out.head_stride);
         const int part_row = (PAIR ? slot * kTileRows : 0) + row;
         const int h0 = PAIR ? 0 : slot * (D / 32), h1 = PAIR ? D / 16 : h0 + D / 32;  // the slots of one row tile share its columns
@@ -1187,7 +1199,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             for (int c = 0; c < 16; ++c) o[c] = z[c];
           }
 #pragma unroll
-          for (int c = 0; c < 16; ++c) o[c] *= inv;  // (NaN if a wait has run out)
+          for (int c = 0; c < 16; ++c) o[c] *= inv;
           if (live) {
             if (whole) {
 #pragma unroll
@@ -1206,7 +1218,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
           if (!whole)
             p.part_ml[((int64_t)blockIdx.x * 2 + (from_start ? 1 : 0)) * S::kItemRows + part_row] = make_float2(r, l * inv);
           else if (p.lse)
-            p.lse[((int64_t)g.b * p.n + t) * p.heads + head] = failed ? inv : l == 0.f ? -INFINITY : kLn2 * (r + log2f(l));
+            p.lse[((int64_t)g.b * p.n + t) * p.heads + head] = l == 0.f ? -INFINITY : kLn2 * (r + log2f(l));
         }
         tc_fence_before();
       }
