@@ -51,8 +51,8 @@ typedef struct {
   int32_t page_size;        /* tokens per page: a power of two, 8 .. 65536 */
   int32_t kv_heads;         /* >= 1 */
   int32_t head_dim;         /* 64 or 128, contiguous */
-  int64_t page_stride;      /* elements from one page, token and head to the next, whole 16-byte units; any order of the three */
-  int64_t token_stride;     /* dimensions (a dimension of one entry may have any stride) */
+  int64_t page_stride;      /* elements from one page, token and head to the next: whole 16-byte units, at least head_dim, any order */
+  int64_t token_stride;     /* of the three dimensions (a dimension of one entry may have any stride) */
   int64_t head_stride;
   const int32_t* block_table; /* dev [sequences, max_pages] page ids, rows table_stride entries apart.  A page id outside
                                  [0, num_pages) is never followed: tokens for it are not written, and it is read as a
@@ -81,7 +81,7 @@ fly_status_t fly_cache_append(const fly_cache_t* cache, int32_t B, int32_t n, co
 
 /* Reads positions starts[b] .. starts[b] + n - 1 of every sequence (starts dev [B], NULL = 0) into k and v [B, n, kv_heads, head_dim].
  * Exact: both formats hold bf16 values.  Rows of positions that sequence b does not hold - negative ones, those from
- * lengths[b] on, and those on a page whose id is out of range - are left as they are. */
+ * lengths[b] on, and those on a page whose id is out of range - are left as they are.  Strides of k and v are at least head_dim. */
 fly_status_t fly_cache_read(const fly_cache_t* cache, int32_t B, int32_t n, const int32_t* starts, const fly_rows_t* k,
                             const fly_rows_t* v, void* cuda_stream);
 
@@ -90,7 +90,10 @@ fly_status_t fly_cache_read(const fly_cache_t* cache, int32_t B, int32_t n, cons
  * them, so append first - and with a window only those with p > P - window or p < sinks:
  *   s_p = scale * <q, k_p>,   lse = ln sum_p e^{s_p},   out = sum_p e^{s_p - lse} v_p.
  * A row that sees nothing, or only scores of -inf, gets out 0 and lse -inf.  Keys and values that a row does not see have no
- * influence on it, whatever they hold.
+ * influence on it, whatever they hold.  Products are added up in fp32 (weights rounded to bf16; over E4M3 a query is
+ * exact down to 2^-17 of the largest of its row and off by 2^-22 of that below), so magnitudes beyond 2^100 may overflow on the way, and
+ * a row with scores beyond 2^30, of whose weights fp32 leaves nothing, may come out as NaN.
+ * out may be q itself; otherwise the two do not overlap.
  *
  * A handle owns the scratch in which the parts of a long context meet, so steps of one handle run one after the other
  * on the GPU (one handle per stream, as in fly_verify.h), and graphs captured with it too. */
@@ -112,7 +115,7 @@ typedef struct {
   int32_t B;              /* 1 .. max_batch, at most cache->sequences */
   int32_t n;              /* 1 .. max_tokens */
   fly_rows_t q;           /* [B, n, heads, head_dim]; 16-byte aligned, strides whole 16-byte units and not 0 */
-  fly_rows_t out;         /* the same shape; rows from counts[b] on are left as they are */
+  fly_rows_t out;         /* the same shape, strides at least head_dim; rows from counts[b] on are left as they are */
   float* lse;             /* dev [B, n, heads] contiguous or NULL */
   const int32_t* counts;  /* dev [B] or NULL */
   int32_t window;         /* 0: everything up to the row's own position; >= 1: the last `window` positions (its own among them) */
@@ -120,6 +123,8 @@ typedef struct {
   double scale;           /* > 0, or 0 for 1 / sqrt(head_dim) */
 } fly_attention_args_t;
 
+/* One kernel, and another one for the parts of long contexts where there may be any.  FLY_ERR_UNSUPPORTED where the sequences' tables
+ * together span more than 2^31 tiles of 128 positions per key/value head and row tile. */
 fly_status_t fly_attention_run(fly_attention_t* handle, const fly_cache_t* cache, const fly_attention_args_t* args,
                                void* cuda_stream);
 

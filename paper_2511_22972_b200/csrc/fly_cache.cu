@@ -52,6 +52,9 @@ fly_status_t check_cache(const fly_cache_t* c, int32_t B, int32_t n) {
     return FLY_ERR_UNSUPPORTED;
   if ((c->num_pages > 1 && c->page_stride % unit) || c->token_stride % unit || (c->kv_heads > 1 && c->head_stride % unit))
     return FLY_ERR_UNSUPPORTED;
+  // (rows that overlap hold nothing)
+  if ((c->num_pages > 1 && c->page_stride < c->head_dim) || c->token_stride < c->head_dim || (c->kv_heads > 1 && c->head_stride < c->head_dim))
+    return FLY_ERR_UNSUPPORTED;
   return FLY_OK;
 }
 
@@ -64,6 +67,11 @@ fly_status_t check_rows(const fly_rows_t* r) {
 bool wide(const fly_rows_t* r, int32_t B, int32_t n, int32_t heads) {
   return aligned(r->data, 16) && (B == 1 || r->batch_stride % 8 == 0) && (n == 1 || r->token_stride % 8 == 0) &&
          (heads == 1 || r->head_stride % 8 == 0);
+}
+
+// Whether no dimension of rows that are written is a broadcast.
+bool apart(const fly_rows_t* r, int32_t B, int32_t n, int32_t heads, int32_t head_dim) {
+  return (B == 1 || r->batch_stride >= head_dim) && (n == 1 || r->token_stride >= head_dim) && (heads == 1 || r->head_stride >= head_dim);
 }
 
 K::View view_of(const fly_cache_t* c) {
@@ -198,6 +206,7 @@ fly_status_t fly_cache_read(const fly_cache_t* c, int32_t B, int32_t n, const in
                             void* cuda_stream) {
   fly_status_t s = check_cache(c, B, n);
   if (s != FLY_OK || (s = check_rows(k)) != FLY_OK || (s = check_rows(v)) != FLY_OK) return s;
+  if (!apart(k, B, n, c->kv_heads, c->head_dim) || !apart(v, B, n, c->kv_heads, c->head_dim)) return FLY_ERR_UNSUPPORTED;
   DeviceGuard g(c->device);
   if (!g.ok) return FLY_ERR_CUDA;
   cudaLaunchConfig_t cfg;
@@ -276,6 +285,7 @@ fly_status_t fly_attention_run(fly_attention_t* h, const fly_cache_t* c, const f
   if (!wide(&a->q, a->B, a->n, heads) || !wide(&a->out, a->B, a->n, heads)) return FLY_ERR_UNSUPPORTED;
   if ((a->B > 1 && a->q.batch_stride == 0) || (a->n > 1 && a->q.token_stride == 0) || (heads > 1 && a->q.head_stride == 0))
     return FLY_ERR_UNSUPPORTED;
+  if (!apart(&a->out, a->B, a->n, heads, D)) return FLY_ERR_UNSUPPORTED;
   DeviceGuard g(h->cfg.device);
   if (!g.ok) return FLY_ERR_CUDA;
   A::Params p;

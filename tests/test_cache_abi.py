@@ -106,3 +106,15 @@ def test_tensors_on_the_host_are_refused_in_python():
         with pytest.raises((ValueError, RuntimeError)):
             Bd._native.attention_run(0, C.addressof(c), 4, bad, bad, 0, 0, 0.0, None, None, 0)
     assert Bd._native.cache_append(0, p, p, None, None, 0) == INVALID
+
+
+@pytest.mark.parametrize("kw", [dict(token_stride=0), dict(token_stride=56), dict(head_stride=0), dict(page_stride=0), dict(page_stride=56)])
+def test_caches_whose_rows_overlap_are_refused(kw):
+    test_caches_that_are_refused(kw, UNSUPPORTED)
+
+
+@pytest.mark.parametrize("strides", [(0, 128, 64), (512, 0, 64), (512, 128, 0), (512, 128, 56)])
+def test_rows_that_are_written_do_not_overlap(strides):
+    L, c, r, ok = cache.lib(), good(), cache.fly_rows_t(A, *strides), cache.fly_rows_t(A, 512, 128, 64)
+    assert L.fly_cache_read(C.byref(c), 2, 4, None, C.byref(r), C.byref(ok), None) == UNSUPPORTED
+    assert L.fly_cache_read(C.byref(c), 2, 4, None, C.byref(ok), C.byref(r), None) == UNSUPPORTED

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from paper_2511_22972_b200 import ChunkAttention, binding as Bd
+from paper_2511_22972_b200 import ChunkAttention, PagedCache, binding as Bd
 from tests._cache import Pool, check_attention, rows
 
 pytestmark = pytest.mark.gpu
@@ -316,3 +316,139 @@ def test_every_form_gives_nan_while_a_wait_that_ran_out_is_pending(fmt, dim, n):
     assert att.device_status(stream()) == Bd.FLY_ERR_TIMEOUT
     assert bool(out.isnan().all()) and bool(lse.isnan().all())
     run(pool, n, 16, handle=att, rows_of={0, n - 1})
+
+
+# ---- values and sizes at the edges ------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("heads,kv_heads,n,dim", [(128, 1, 1, 128), (127, 1, 2, 64), (128, 1, 3, 64), (65, 1, 3, 128), (3, 1, 50, 64), (15, 5, 9, 128), (100, 2, 2, 64)])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_groups_of_all_sizes(fmt, heads, kv_heads, n, dim):
+    run(held([0, 130, 300], n, kv_heads, dim, 32, fmt, seed=heads), n, heads, seed=n, rows_of={0, n // 2, n - 1})
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("lengths", [[500], [511], [512], [513], [480, 0, 100, 505], [300] * 32, [300] * 33, [500] * 80, [600] + [10] * 60])
+def test_whole_items_and_cut_ones(fmt, lengths):
+    # around four tiles of positions, 32 groups, one item to an SM
+    pool = held(lengths, 3, 2, 64, 16, fmt, seed=len(lengths))
+    run(pool, 3, 4, rows_of={2})
+    run(pool, 3, 4, 200, 20, rows_of={0})
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("n", [5, 50])
+@pytest.mark.parametrize("window,sinks", [(10, 5), (40, 60), (3, 130), (200, 1)])
+def test_first_tokens_and_window_in_one_tile(fmt, n, window, sinks):
+    run(held([0, 20, 90, 100, 126, 140, 250, 270], n, 1, 64, 16, fmt, seed=window), n, 8, window, sinks, rows_of=set(range(0, n, 7)) | {n - 1})
+
+
+@pytest.mark.parametrize("n", [4, 40])
+def test_scales_and_codes_that_append_does_not_write(n):
+    # values' scales over the whole range, NaN codes where nobody looks (a page's slots past the end are full of them already)
+    pool = held([200, 333], n, 2, 64, 16, "e4m3", seed=3)
+    s = pool.v_scales.cpu()
+    g = torch.Generator().manual_seed(3)
+    live = s != 255
+    s[live] = torch.tensor([0, 1, 6, 7, 100, 133, 134, 135, 136, 180, 220], dtype=torch.uint8)[torch.randint(11, (int(live.sum()),), generator=g)]
+    pool.v_scales.copy_(s)
+    run(pool, n, 8, rows_of={0, n - 1})
+    run(pool, n, 8, 50, 20, rows_of={0, n - 1})
+
+
+def test_e4m3_queries_of_a_wide_range():
+    # what is far below the largest value of a query row is kept to 2^-22 of that value
+    n = 9
+    pool = held([300, 20], n, 2, 64, 16, "e4m3", seed=8)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    q = rows(2, n, 8, 64, g)
+    q *= torch.exp2(torch.randint(-30, 3, q.shape, generator=g, device="cuda").float()).bfloat16()
+    q[0, 0] = 0
+    q[1, 2] *= 2.0 ** -100
+    q[1, 3, 1] = torch.finfo(torch.bfloat16).tiny
+    run(pool, n, 8, q=q)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("n", [3, 40])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_queries_that_are_not_finite_stay_in_their_rows(fmt, n, bad):
+    pool = held([300, 20], n, 2, 64, 16, fmt, seed=8)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    q = rows(2, n, 8, 64, g)
+    _, good, good_lse = run(pool, n, 8, q=q, rows_of={0})
+    q = q.clone()
+    q[0, 1, 3, 17] = bad
+    q[1, n - 1, 0] = bad
+    out, lse, att = torch.zeros_like(q), torch.zeros_like(good_lse), ChunkAttention(2, n, 8, 2, 64)
+    att.run(pool.cache, q, out, lse=lse, stream=stream())
+    hit = torch.zeros(2, n, 8, dtype=torch.bool, device="cuda")
+    hit[0, 1, 3] = hit[1, n - 1, 0] = True
+    assert bool(out[hit].isnan().all()) and bool(lse[hit].isnan().all())
+    assert torch.equal(out[~hit], good[~hit]) and torch.equal(lse[~hit], good_lse[~hit])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("lengths,n", [([700, 20], 4), ([5000], 3), ([300, 100], 60)])
+def test_the_output_may_be_the_queries(fmt, lengths, n):
+    pool = held(lengths, n, 2, 64, 16, fmt, seed=4)
+    q, want, _ = run(pool, n, 16, 0, 0, rows_of={0})
+    both, att = q.clone(), ChunkAttention(len(lengths), n, 16, 2, 64)
+    att.run(pool.cache, both, both, stream=stream())
+    assert torch.equal(both, want)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_pages_past_32_bits(fmt):
+    # three pages 2^30 elements (bf16) or 2^31 (e4m3) apart
+    n, H, D, page, step = 3, 2, 64, 64, 2 ** (30 if fmt == "bf16" else 31)
+    small = held([150], n, H, D, page, fmt, spare=0, seed=7)
+    flat = [torch.zeros(2 * step + page * H * D, dtype=small.k_pages.dtype, device="cuda") for _ in "kv"]
+    for t, x in zip(flat, (small.k_pages, small.v_pages)):
+        big = t.as_strided((3, page, H, D), (step, H * D, D, 1))
+        (big.view(torch.uint8) if fmt == "e4m3" else big).copy_(x.view(torch.uint8) if fmt == "e4m3" else x)
+    k, v = (t.as_strided((3, page, H, D), (step, H * D, D, 1)) for t in flat)
+    small.k_pages, small.v_pages = k, v
+    small.cache = PagedCache(k, v, small.d_table, small.d_lengths, small.k_scales, small.v_scales)
+    run(small, n, 8)
+
+
+def test_two_handles_on_two_streams():
+    pools = [held([3000, 100], 5, 2, 64, 16, f, seed=3) for f in FORMATS]
+    g = torch.Generator(device="cuda").manual_seed(1)
+    qs, atts, side = [rows(2, 5, 16, 64, g) for _ in pools], [ChunkAttention(2, 5, 16, 2, 64) for _ in pools], [torch.cuda.Stream() for _ in pools]
+    outs, lses = [[torch.zeros_like(qs[0]) for _ in range(20)] for _ in pools], [torch.zeros(2, 5, 16, device="cuda") for _ in pools]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for k in range(2):
+            atts[k].run(pools[k].cache, qs[k], outs[k][i], lse=lses[k], stream=side[k].cuda_stream)
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert all(torch.equal(o, outs[k][0]) for o in outs[k])
+        check_attention(pools[k], qs[k], outs[k][0], lses[k], rows_of={0, 4})
+
+
+def test_tables_of_too_many_tiles_are_refused():
+    # 2^30 positions in each of 200 sequences: more tiles than the schedule counts
+    pages = torch.zeros(1, 65536, 2, 64, dtype=torch.bfloat16, device="cuda")
+    table = torch.zeros(200, 16384, dtype=torch.int32, device="cuda")
+    lengths = torch.zeros(200, dtype=torch.int32, device="cuda")
+    cache = PagedCache(pages, pages, table, lengths)
+    q = torch.zeros(200, 1, 2, 64, dtype=torch.bfloat16, device="cuda")
+    att = ChunkAttention(200, 1, 2, 2, 64)
+    with pytest.raises(Bd.FlyError) as e:
+        att.run(cache, q, torch.zeros_like(q), stream=stream())
+    assert e.value.status == Bd.FLY_ERR_UNSUPPORTED
+    for bad in (q[:, :, :1].expand(200, 1, 2, 64), q[:1].expand(200, 1, 2, 64)):     # an output of which several rows are one
+        with pytest.raises(Bd.FlyError) as e:
+            att.run(cache, q, bad, stream=stream())
+        assert e.value.status == Bd.FLY_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("scale", [2.0 ** 16, 2.0 ** 20, 2.0 ** 22])
+def test_scores_whose_ulps_are_large(fmt, scale):
+    # (up to 2^30, beyond which the header promises nothing)
+    for n, heads in ((9, 4), (70, 4)):
+        pool = held([300, 20], n, 1, 64, 16, fmt, seed=8)
+        run(pool, n, heads, scale=scale, rows_of={0, n - 1})
+        run(pool, n, heads, 50, 3, scale=scale, rows_of={0, n - 1})
