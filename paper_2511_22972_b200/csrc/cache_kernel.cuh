@@ -171,73 +171,61 @@ __device__ __forceinline__ uint32_t amax2(uint32_t a, uint32_t b) {  // of two p
   return __vmaxu2(a & 0x7fff7fffu, b & 0x7fff7fffu);
 }
 
-// Threads of a block, and rows of a lane group taken together so that their loads are in flight together.  us, rows at a time: append 3 x 4099
-// tokens of 8 heads 1: 15.7 (blocks of 256 threads 16.8), 2: 19.7; read 8 x 4 - 16 k tokens 1: 102.4, 2: 101.9, 4: 96.1 (blocks of 128
-// threads 98.9), 8: 103.
-constexpr int kAppendThreads = 128, kReadThreads = 256, kAppendRows = 1, kReadRows = 4;
+// Threads of a block, and rows of a lane group read together so that their loads are in flight together.  us, rows at a time: append 3 x 4099
+// tokens of 8 heads x 128 to e4m3 1: 15.7 = 4.8 TB/s (blocks of 256 threads 16.8), 2: 19.7; read 8 x 4 - 16 k tokens of 8 heads x 128 from e4m3
+// 1: 102.4, 2: 101.9, 4: 96.1 = 5.1 TB/s (blocks of 128 threads 98.9), 8: 103.
+constexpr int kAppendThreads = 128, kReadThreads = 256, kReadRows = 4;
 
 // A group of D / 16 lanes per (sequence, token, head), sixteen values of the key and sixteen of the value per lane.  What bounds these kernels is
 // bytes, or for small calls the chain length -> page -> row.
-template <int D, bool E4M3, int ROWS>
+template <int D, bool E4M3>
 __global__ void __launch_bounds__(kAppendThreads) append_kernel(const View c, const Rows k, const Rows v, int B, int n, const int32_t* counts,
                                                           uint32_t* row_flags, int wide) {
   constexpr int kLanes = D / 16, kGroups = kAppendThreads / kLanes;
   asm volatile("griddepcontrol.wait;" ::: "memory");  // the kernel before may have written any of the inputs
   asm volatile("griddepcontrol.launch_dependents;");
   const int lane = (int)threadIdx.x % kLanes;
-  const uint32_t row0 = blockIdx.x * (kGroups * ROWS) + threadIdx.x / kLanes, rows = (uint32_t)n * (uint32_t)c.kv_heads;
+  const uint32_t row = blockIdx.x * kGroups + threadIdx.x / kLanes, rows = (uint32_t)n * (uint32_t)c.kv_heads;
+  const int token = (int)(row / (uint32_t)c.kv_heads), head = (int)(row - (uint32_t)token * (uint32_t)c.kv_heads);
   const unsigned group = ((1u << kLanes) - 1u) << ((threadIdx.x & 31) / kLanes * kLanes);
   for (int b = (int)blockIdx.y; b < B; b += (int)gridDim.y) {
     const int count = count_of(counts, b, n), L = length_of(c, b);
-    uint4 x[ROWS][2][2];
-    int page[ROWS], token[ROWS], head[ROWS];
-    bool mine[ROWS];
+    if (row >= rows || token >= count) continue;  // (whole groups)
+    const int page = L < 0 || (int64_t)L + token >= c.capacity ? -1 : page_of(c, b, L + token);
+    uint4 x[2][2];  // (the rows need no page)
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {  // (the rows need no page)
-      const uint32_t row = row0 + r * kGroups;
-      token[r] = (int)(row / (uint32_t)c.kv_heads);
-      head[r] = (int)(row - (uint32_t)token[r] * (uint32_t)c.kv_heads);
-      mine[r] = row < rows && token[r] < count;
-      if (!mine[r]) continue;
-      page[r] = L < 0 || (int64_t)L + token[r] >= c.capacity ? -1 : page_of(c, b, L + token[r]);
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const Rows& src = t ? v : k;
-        const uint8_t* from = src.data + 2 * ((int64_t)b * src.batch_stride + (int64_t)token[r] * src.token_stride + (int64_t)head[r] * src.head_stride + lane * 16);
-        x[r][t][0] = load8(from, (wide >> t) & 1);
-        x[r][t][1] = load8(from + 16, (wide >> t) & 1);
-      }
+    for (int t = 0; t < 2; ++t) {
+      const Rows& src = t ? v : k;
+      const uint8_t* from = src.data + 2 * ((int64_t)b * src.batch_stride + (int64_t)token * src.token_stride + (int64_t)head * src.head_stride + lane * 16);
+      x[t][0] = load8(from, (wide >> t) & 1);
+      x[t][1] = load8(from + 16, (wide >> t) & 1);
     }
+    if (row_flags && lane == 0 && head == 0) row_flags[(int64_t)b * n + token] = page < 0 ? kFlagNotWritten : 0u;
+    if (page < 0) continue;
+    const int slot = (L + token) & ((1 << c.page_shift) - 1);
+    const int64_t at = row_at(c, page, slot, head) + lane * 16;
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-      if (!mine[r]) continue;  // (whole groups)
-      if (row_flags && lane == 0 && head[r] == 0) row_flags[(int64_t)b * n + token[r]] = page[r] < 0 ? kFlagNotWritten : 0u;
-      if (page[r] < 0) continue;
-      const int slot = (L + token[r]) & ((1 << c.page_shift) - 1);
-      const int64_t at = row_at(c, page[r], slot, head[r]) + lane * 16;
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        uint8_t* pages = t ? c.v_pages : c.k_pages;
-        const uint4 y = x[r][t][0], z = x[r][t][1];
-        if (!E4M3) {
-          *reinterpret_cast<uint4*>(pages + 2 * at) = y;
-          *reinterpret_cast<uint4*>(pages + 2 * at + 16) = z;
-          continue;
-        }
-        const uint32_t m2 = __vmaxu2(__vmaxu2(amax2(y.x, y.y), amax2(y.z, y.w)), __vmaxu2(amax2(z.x, z.y), amax2(z.z, z.w)));
-        uint32_t m = max(m2 & 0xffffu, m2 >> 16);
-        m = __reduce_max_sync(group, m);
-        const int s = scale_of(m);
-        const float inv = __uint_as_float((uint32_t)(254 - s) << 23);
-        uint4 codes = make_uint4(0u, 0u, 0u, 0u);
-        if (s != kScaleNan)
-          codes = make_uint4(pack_e4m3(bf16_lo(y.x) * inv, bf16_hi(y.x) * inv, bf16_lo(y.y) * inv, bf16_hi(y.y) * inv),
-                             pack_e4m3(bf16_lo(y.z) * inv, bf16_hi(y.z) * inv, bf16_lo(y.w) * inv, bf16_hi(y.w) * inv),
-                             pack_e4m3(bf16_lo(z.x) * inv, bf16_hi(z.x) * inv, bf16_lo(z.y) * inv, bf16_hi(z.y) * inv),
-                             pack_e4m3(bf16_lo(z.z) * inv, bf16_hi(z.z) * inv, bf16_lo(z.w) * inv, bf16_hi(z.w) * inv));
-        *reinterpret_cast<uint4*>(pages + at) = codes;
-        if (lane == 0) (t ? c.v_scales : c.k_scales)[scale_at(c, page[r], slot, head[r])] = (uint8_t)s;
+    for (int t = 0; t < 2; ++t) {
+      uint8_t* pages = t ? c.v_pages : c.k_pages;
+      const uint4 y = x[t][0], z = x[t][1];
+      if (!E4M3) {
+        *reinterpret_cast<uint4*>(pages + 2 * at) = y;
+        *reinterpret_cast<uint4*>(pages + 2 * at + 16) = z;
+        continue;
       }
+      const uint32_t m2 = __vmaxu2(__vmaxu2(amax2(y.x, y.y), amax2(y.z, y.w)), __vmaxu2(amax2(z.x, z.y), amax2(z.z, z.w)));
+      uint32_t m = max(m2 & 0xffffu, m2 >> 16);
+      m = __reduce_max_sync(group, m);
+      const int s = scale_of(m);
+      const float inv = __uint_as_float((uint32_t)(254 - s) << 23);
+      uint4 codes = make_uint4(0u, 0u, 0u, 0u);
+      if (s != kScaleNan)
+        codes = make_uint4(pack_e4m3(bf16_lo(y.x) * inv, bf16_hi(y.x) * inv, bf16_lo(y.y) * inv, bf16_hi(y.y) * inv),
+                           pack_e4m3(bf16_lo(y.z) * inv, bf16_hi(y.z) * inv, bf16_lo(y.w) * inv, bf16_hi(y.w) * inv),
+                           pack_e4m3(bf16_lo(z.x) * inv, bf16_hi(z.x) * inv, bf16_lo(z.y) * inv, bf16_hi(z.y) * inv),
+                           pack_e4m3(bf16_lo(z.z) * inv, bf16_hi(z.z) * inv, bf16_lo(z.w) * inv, bf16_hi(z.w) * inv));
+      *reinterpret_cast<uint4*>(pages + at) = codes;
+      if (lane == 0) (t ? c.v_scales : c.k_scales)[scale_at(c, page, slot, head)] = (uint8_t)s;
     }
   }
 }
