@@ -678,6 +678,15 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(base + S::kOffMisc) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  if (!E4M3) {
+    // Rows of a tile that no box brings: products with zeros take less power, and loops of 64 sequences of one token run into the limit (1 kW: 215 - 230 us,
+    // with zeros 202 - 214; the first 50 ms 186, 184).  (E4M3: the softmax warps write zeros themselves.)
+    const int rows = p.tpt * p.group;
+    for (int i = tid; i < (kTileRows - rows) * 8; i += S::kThreads)
+#pragma unroll
+      for (int h = 0; h < S::kQBufs * S::kHalves; ++h) *reinterpret_cast<uint4*>(smem + h * S::kHalfBytes + rows * 128 + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+    async_proxy_fence();
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
