@@ -1302,7 +1302,7 @@ __global__ void __launch_bounds__(kCombineThreads) attention_combine_kernel(cons
       const int k = (int)(u / per_item), in = (int)(u - (int64_t)k * per_item), col4 = in / rows, row = in - col4 * rows;
       const int4 a = list[k][0], e = list[k][1];
       const int c = e.w, x0 = a.x, count = a.y, share = a.z, kvh = a.w, b = e.x, t0 = e.y, t1 = e.z;
-      const int parts = 1 + (count - x0 + share - 1) / share;
+      const int parts = min(1 + (count - x0 + share - 1) / share, ctas - c + 1);  // (the bound: whatever lengths do meanwhile)
       const int slot = row / kTileRows, in_slot = row - slot * kTileRows, token = in_slot / p.group;
       const int t = t0 + slot * p.tpt + token;
       if (token >= p.tpt || t >= t1) continue;

@@ -48,6 +48,7 @@ fly_status_t check_cache(const fly_cache_t* c, int32_t B, int32_t n) {
   if (c->page_size < 8 || c->page_size > 65536 || (c->page_size & (c->page_size - 1)) != 0) return FLY_ERR_UNSUPPORTED;
   if ((int64_t)c->max_pages * c->page_size > (int64_t)1 << 30 || n > kMaxTokens) return FLY_ERR_UNSUPPORTED;
   const int64_t unit = e4m3 ? 16 : 8;  // elements in 16 bytes
+  if (!aligned(c->block_table, 4) || !aligned(c->lengths, 4)) return FLY_ERR_UNSUPPORTED;
   if (!aligned(c->k_pages, 16) || !aligned(c->v_pages, 16) || (e4m3 && (!aligned(c->k_scales, 8) || !aligned(c->v_scales, 8))))
     return FLY_ERR_UNSUPPORTED;
   if ((c->num_pages > 1 && c->page_stride % unit) || c->token_stride % unit || (c->kv_heads > 1 && c->head_stride % unit))
@@ -162,8 +163,9 @@ cudaError_t launch(fly_attention* h, const CUtensorMap* maps, const A::Params& p
   fill_launch(&cfg, attr, (unsigned)h->sm_count, S::kThreads, st, true);
   cfg.dynamicSmemBytes = S::kSmem;
   cudaError_t e = cudaLaunchKernelEx(&cfg, A::attention_kernel<D, E4M3, PAIR>, maps[0], maps[1], maps[2], p);
-  if (e != cudaSuccess || h->sm_count < 2) return e;
+  if (e != cudaSuccess) return e;
   h->last_launches++;
+  if (h->sm_count < 2) return e;
   // (one kernel less: a context of 300 positions 12.0 -> 10.6 us) Nothing is cut where every item is short enough to stay whole, whatever the lengths are.
   if (p.groups <= 32 && (int64_t)p.groups * p.c.kv_heads <= h->sm_count && p.c.capacity <= A::kWholeItem * A::kTile) return e;
   // (blocks for as many cut items as there can be, at most four per SM)
@@ -183,6 +185,7 @@ fly_status_t fly_cache_append(const fly_cache_t* c, int32_t B, int32_t n, const 
                               const int32_t* counts, uint32_t* row_flags, void* cuda_stream) {
   fly_status_t s = check_cache(c, B, n);
   if (s != FLY_OK || (s = check_rows(k)) != FLY_OK || (s = check_rows(v)) != FLY_OK) return s;
+  if (!aligned(counts, 4) || !aligned(row_flags, 4)) return FLY_ERR_UNSUPPORTED;
   DeviceGuard g(c->device);
   if (!g.ok) return FLY_ERR_CUDA;
   cudaLaunchConfig_t cfg;
@@ -203,7 +206,7 @@ fly_status_t fly_cache_read(const fly_cache_t* c, int32_t B, int32_t n, const in
                             void* cuda_stream) {
   fly_status_t s = check_cache(c, B, n);
   if (s != FLY_OK || (s = check_rows(k)) != FLY_OK || (s = check_rows(v)) != FLY_OK) return s;
-  if (!apart(k, B, n, c->kv_heads, c->head_dim) || !apart(v, B, n, c->kv_heads, c->head_dim)) return FLY_ERR_UNSUPPORTED;
+  if (!aligned(starts, 4) || !apart(k, B, n, c->kv_heads, c->head_dim) || !apart(v, B, n, c->kv_heads, c->head_dim)) return FLY_ERR_UNSUPPORTED;
   DeviceGuard g(c->device);
   if (!g.ok) return FLY_ERR_CUDA;
   cudaLaunchConfig_t cfg;
@@ -282,7 +285,7 @@ fly_status_t fly_attention_run(fly_attention_t* h, const fly_cache_t* c, const f
   if (!wide(&a->q, a->B, a->n, heads) || !wide(&a->out, a->B, a->n, heads)) return FLY_ERR_UNSUPPORTED;
   if ((a->B > 1 && a->q.batch_stride == 0) || (a->n > 1 && a->q.token_stride == 0) || (heads > 1 && a->q.head_stride == 0))
     return FLY_ERR_UNSUPPORTED;
-  if (!apart(&a->out, a->B, a->n, heads, D)) return FLY_ERR_UNSUPPORTED;
+  if (!aligned(a->counts, 4) || !aligned(a->lse, 4) || !apart(&a->out, a->B, a->n, heads, D)) return FLY_ERR_UNSUPPORTED;
   DeviceGuard g(h->cfg.device);
   if (!g.ok) return FLY_ERR_CUDA;
   A::Params p;

@@ -51,7 +51,7 @@ CACHES = [
     (dict(token_stride=-128), INVALID), (dict(head_dim=80), UNSUPPORTED), (dict(head_dim=256), UNSUPPORTED), (dict(page_size=4), UNSUPPORTED),
     (dict(page_size=24), UNSUPPORTED), (dict(page_size=131072), UNSUPPORTED), (dict(max_pages=1 << 27, table_stride=1 << 27), UNSUPPORTED),
     (dict(k_pages=A + 8), UNSUPPORTED), (dict(page_stride=2052), UNSUPPORTED), (dict(token_stride=132), UNSUPPORTED), (dict(head_stride=68), UNSUPPORTED),
-    (dict(format=1, k_scales=A + 4, v_scales=A), UNSUPPORTED), (dict(format=1, k_scales=A, v_scales=A, head_stride=72), UNSUPPORTED),
+    (dict(block_table=A + 2), UNSUPPORTED), (dict(lengths=A + 1), UNSUPPORTED), (dict(format=1, k_scales=A + 4, v_scales=A), UNSUPPORTED), (dict(format=1, k_scales=A, v_scales=A, head_stride=72), UNSUPPORTED),
 ]
 
 
@@ -118,3 +118,10 @@ def test_rows_that_are_written_do_not_overlap(strides):
     L, c, r, ok = cache.lib(), good(), cache.fly_rows_t(A, *strides), cache.fly_rows_t(A, 512, 128, 64)
     assert L.fly_cache_read(C.byref(c), 2, 4, None, C.byref(r), C.byref(ok), None) == UNSUPPORTED
     assert L.fly_cache_read(C.byref(c), 2, 4, None, C.byref(ok), C.byref(r), None) == UNSUPPORTED
+
+
+def test_device_integers_off_their_alignment_are_refused():
+    L, c, r = cache.lib(), good(), cache.fly_rows_t(A, 512, 128, 64)
+    assert L.fly_cache_append(C.byref(c), 2, 4, C.byref(r), C.byref(r), A + 1, None, None) == UNSUPPORTED
+    assert L.fly_cache_append(C.byref(c), 2, 4, C.byref(r), C.byref(r), None, A + 2, None) == UNSUPPORTED
+    assert L.fly_cache_read(C.byref(c), 2, 4, A + 3, C.byref(r), C.byref(r), None) == UNSUPPORTED

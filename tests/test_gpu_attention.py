@@ -452,3 +452,16 @@ def test_scores_whose_ulps_are_large(fmt, scale):
         pool = held([300, 20], n, 1, 64, 16, fmt, seed=8)
         run(pool, n, heads, scale=scale, rows_of={0, n - 1})
         run(pool, n, heads, 50, 3, scale=scale, rows_of={0, n - 1})
+
+
+def test_pointers_off_their_alignment_are_refused():
+    import ctypes as C
+    from paper_2511_22972_b200 import cache as M
+    pool = held([10, 20], 4, 2, 64)
+    att, g = ChunkAttention(2, 4, 8, 2, 64), torch.Generator(device="cuda").manual_seed(8)
+    q, lse = rows(2, 4, 8, 64, g), torch.zeros(2 * 4 * 8 + 1, device="cuda")
+    r = M.fly_rows_t(q.data_ptr(), *q.stride()[:3])
+    for counts, at, want in ((None, 0, Bd.FLY_OK), (None, 2, Bd.FLY_ERR_UNSUPPORTED), (pool.d_lengths.data_ptr() + 1, 0, Bd.FLY_ERR_UNSUPPORTED)):
+        a = M.fly_attention_args_t(2, 4, r, r, lse.data_ptr() + at, counts, 0, 0, 0.0)
+        assert M.lib().fly_attention_run(att._h, C.byref(pool.cache.struct), C.byref(a), C.c_void_p(stream())) == want
+    torch.cuda.synchronize()
