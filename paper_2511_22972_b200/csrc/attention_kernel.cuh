@@ -576,11 +576,13 @@ __device__ __forceinline__ void softmax_blocks(uint32_t ts, uint32_t to, float s
   sum += x + y;
 }
 
-// Adds back to a row what zero_nonfinite took out of the values that it sees; columns col0 .. col0 + 15 of row_pos are in o.
+// Adds back to a row what zero_nonfinite took out of the values that it sees at positions from .. to - 1; columns col0 .. col0 + 15 of row_pos are in o.
+// (Only those of the tiles that O was formed from: elsewhere the row's reference may be -inf, and where an item's parts meet
+// its O would count 2^-inf times infinity, which is NaN.)
 template <bool E4M3>
-__device__ __noinline__ void add_back(const Params& p, int b, int kvh, int row_pos, int lo_first, int lo_last, int upper, int hi, int col0, float* o) {
-  auto visit = [&](int from, int to) {
-    for (int pos = from; pos < to; ++pos) {
+__device__ __noinline__ void add_back(const Params& p, int b, int kvh, int row_pos, int lo_first, int lo_last, int upper, int hi, int from, int to, int col0, float* o) {
+  auto visit = [&](int first, int last) {
+    for (int pos = max(first, from); pos < min(last, to); ++pos) {
       if (!visible(p, row_pos, pos)) continue;
       const int page = cache::page_of(p.c, b, pos);
       if (page < 0) continue;
@@ -1185,6 +1187,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         tc_fence_after();
       }
       const bool poison = misc[8 + (item & 7)] == item + 1;  // (read when both slots are done where they share the item)
+      // The positions of these tiles from the window on (what only some rows see is never among the first tokens' tiles).
+      const int back0 = (g.lo_tile + max(walk.x0 - g.ns, 0)) * kTile, back1 = (g.lo_tile + walk.x1 - g.ns) * kTile;
       const int head = walk.kvh * p.group + row_head;
       if (failed) {
         if (live) {
@@ -1209,7 +1213,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             float z[16];
 #pragma unroll
             for (int c = 0; c < 16; ++c) z[c] = o[c];
-            add_back<E4M3>(p, g.b, walk.kvh, row_pos, g.lo_first, g.lo_last, min(g.L + g.t0 + 1, g.hi), g.hi, h * 16, z);
+            add_back<E4M3>(p, g.b, walk.kvh, row_pos, g.lo_first, g.lo_last, min(g.L + g.t0 + 1, g.hi), g.hi, back0, back1, h * 16, z);
 #pragma unroll
             for (int c = 0; c < 16; ++c) o[c] = z[c];
           }
