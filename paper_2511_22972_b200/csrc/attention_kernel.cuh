@@ -54,6 +54,9 @@ constexpr int kTile = 128;      // positions per step
 constexpr int kTileRows = 128;  // rows per slot
 constexpr int kErrAttention = 5;
 __device__ __forceinline__ float quiet_nan() { return __uint_as_float(0x7fc00000u); }
+// A factor of scores that fp32 may have rounded to 0: positions that are not seen have scores of -inf, and 0 * -inf is NaN.  The smallest fp32 number
+// in its place is off by at most 2^-149, 2^-21 on scores of up to 2^128.
+__host__ __device__ __forceinline__ float positive(float x) { return x > 0.f ? x : 1.401298464324817e-45f; }
 
 struct Params {
   cache::View c;
@@ -62,7 +65,7 @@ struct Params {
   const int32_t* counts;
   int B, n, heads, group;  // group: query heads per key/value head
   int window, sinks;       // window 0: none
-  float scale;             // log2(e) * the softmax's scale
+  float scale;             // log2(e) * the softmax's scale, > 0
   int tpt;                 // tokens per row tile
   int tpi;                 // tokens per item
   int rt;                  // items per sequence and key/value head
@@ -1079,7 +1082,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
           amax = max(amax, __float_as_uint(exchange[(slot ^ 1) * kTileRows + row].x));
         }
         const int s = cache::scale_of(amax);
-        scale *= cache::scale_value(s);  // (NaN: the row is)
+        if (s == cache::kScaleNan) scale = quiet_nan();  // (so the row is)
+        else scale = positive(scale * cache::scale_value(s));
         const float inv = s == cache::kScaleNan ? 0.f : __uint_as_float((uint32_t)(254 - s) << 23);
         uint8_t* hi = smem + (PAIR ? slot * S::kTileBytes : 0);
 #pragma unroll 1

@@ -302,7 +302,7 @@ fly_status_t fly_attention_run(fly_attention_t* h, const fly_cache_t* c, const f
   const bool window = a->window > 0 && (int64_t)a->window < (int64_t)p.c.capacity + a->n;
   p.window = window ? a->window : 0;
   p.sinks = window ? (a->sinks < p.c.capacity ? a->sinks : p.c.capacity) : 0;
-  p.scale = (float)((a->scale == 0.0 ? 1.0 / std::sqrt((double)D) : a->scale) * 1.4426950408889634);
+  p.scale = A::positive((float)((a->scale == 0.0 ? 1.0 / std::sqrt((double)D) : a->scale) * 1.4426950408889634));
   const int most = A::kTileRows / p.group;  // whole tokens in a row tile
   const bool pair = a->n > most;
   p.tpt = a->n < most ? a->n : most;
