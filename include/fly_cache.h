@@ -120,7 +120,7 @@ typedef struct {
   const int32_t* counts;  /* dev [B] or NULL */
   int32_t window;         /* 0: everything up to the row's own position; >= 1: the last `window` positions (its own among them) */
   int32_t sinks;          /* >= 0: first positions that stay visible; only with a window */
-  double scale;           /* > 0, or 0 for 1 / sqrt(head_dim) */
+  double scale;           /* > 0 and at most 2^127, or 0 for 1 / sqrt(head_dim) */
 } fly_attention_args_t;
 
 /* One kernel, and another one for the parts of long contexts where there may be any.  FLY_ERR_UNSUPPORTED where the sequences' tables

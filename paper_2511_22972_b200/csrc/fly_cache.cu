@@ -282,6 +282,7 @@ fly_status_t fly_attention_run(fly_attention_t* h, const fly_cache_t* c, const f
     return FLY_ERR_INVALID_ARG;
   if (a->window < 0 || a->sinks < 0 || (a->sinks > 0 && a->window == 0)) return FLY_ERR_INVALID_ARG;
   if (!(a->scale >= 0.0) || !std::isfinite(a->scale)) return FLY_ERR_INVALID_ARG;
+  if (a->scale > 0x1p127) return FLY_ERR_UNSUPPORTED;  // (infinite in fp32, times log2(e); a score of 0 would become NaN)
   if (!wide(&a->q, a->B, a->n, heads) || !wide(&a->out, a->B, a->n, heads)) return FLY_ERR_UNSUPPORTED;
   if ((a->B > 1 && a->q.batch_stride == 0) || (a->n > 1 && a->q.token_stride == 0) || (heads > 1 && a->q.head_stride == 0))
     return FLY_ERR_UNSUPPORTED;

@@ -20,3 +20,14 @@ def test_scales_that_leave_nothing_of_the_scores(fmt, n, scale):
     q[1, n - 1, 3] = 0
     run(pool, n, 8, scale=scale, q=q, rows_of={0, n - 1})
     run(pool, n, 8, 40, 3, scale=scale, q=q, rows_of={0, n - 1})
+
+
+@pytest.mark.parametrize("scale", [2.5e38, 1e39, 1e300])
+def test_scales_beyond_fp32_are_refused(scale):
+    # (a score of 0 times infinity would be NaN)
+    pool = held([20], 2, 2, 64)
+    q, att = torch.zeros(1, 2, 8, 64, dtype=torch.bfloat16, device="cuda"), ChunkAttention(1, 2, 8, 2, 64)
+    with pytest.raises(Bd.FlyError) as e:
+        att.run(pool.cache, q, torch.zeros_like(q), scale=scale, stream=stream())
+    assert e.value.status == Bd.FLY_ERR_UNSUPPORTED
+    run(pool, 2, 8, q=q, scale=2.0 ** 127)
