@@ -35,9 +35,9 @@ extern "C" {
  * BF16  as they are.
  * E4M3  one byte a value, and one byte of scale per token, head and tensor: value = code * 2^(scale - 127).  A row of head_dim values
  *       is written with the smallest scale >= 7 for which its largest magnitude does not exceed 448 * 2^(scale - 127), every
- *       value rounded to the nearest code (ties to even).  The scale is a power of two, so scaling rounds nothing, and what
- *       is read back (and what attention computes with) is exact in bf16.  A row that holds a NaN or an infinity gets
- *       scale 255 and reads back as NaN. */
+ *       value rounded to the nearest code (ties to even; with scale 247, the largest, to at most 240, since 256 * 2^120 is not
+ *       a bf16 number).  The scale is a power of two, so scaling rounds nothing, and what is read back (and what attention
+ *       computes with) is exact in bf16.  A row that holds a NaN or an infinity gets scale 255 and reads back as NaN. */
 typedef enum { FLY_CACHE_BF16 = 0, FLY_CACHE_E4M3 = 1 } fly_cache_format_t;
 
 typedef struct {

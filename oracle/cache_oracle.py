@@ -35,7 +35,8 @@ def quantise_row(x) -> tuple[np.ndarray, int]:
     s = 7
     while np.abs(x).max() > 448 * 2.0 ** (s - 127):
         s += 1
-    return np.array([to_code(v / 2.0 ** (s - 127)) for v in x]), s
+    most = 240.0 if s == 247 else 448.0        # (256 * 2^120 is no bf16 number)
+    return np.clip([to_code(v / 2.0 ** (s - 127)) for v in x], -most, most), s
 
 
 def row_values(codes, s: int) -> np.ndarray:

@@ -2,7 +2,9 @@
 //
 // A row is the head_dim values of one token, head and tensor.  BF16 holds them as they are.  E4M3 holds codes c and one scale
 // byte s, value = c * 2^(s - 127): with a power of two as scale the only rounding is that of a value to its code, and every value that
-// is held is a bf16 number (four significant bits, exponent far inside the range), so reading back is exact.
+// is held is a bf16 number, so reading back is exact: it has four significant bits, is a multiple of 2^-129 (the smallest code at the
+// smallest scale; bf16 goes down to 2^-133) and below 2^128.  The last takes care: with the largest scale, 2^120, code 256 would
+// stand for 2^128, so magnitudes from 248 * 2^120 on are held as 240 * 2^120, the nearest value that there is.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -14,6 +16,7 @@ namespace cache {
 constexpr uint32_t kFlagNotWritten = 32u;  // row_flags bit 5
 constexpr int kScaleBias = 127;
 constexpr int kScaleMin = 7;               // 2^-120: what is held stays exact in bf16
+constexpr int kScaleTop = 247;             // of the largest bf16 numbers: codes from 256 on are not finite
 constexpr int kScaleNan = 255;
 
 struct View {
@@ -81,6 +84,8 @@ __device__ __forceinline__ uint32_t pack_e4m3(float x0, float x1, float x2, floa
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(b) : "f"(x3), "f"(x2));
   return (uint32_t)a | ((uint32_t)b << 16);
 }
+// Four codes of up to 256, of which 256 (0x78) becomes 240 (0x77).
+__device__ __forceinline__ uint32_t below_256(uint32_t w) { return w - (__vcmpeq4(w & 0x7f7f7f7fu, 0x78787878u) & 0x01010101u); }
 // Two codes as fp32 (every code is an fp16 number).
 __device__ __forceinline__ void unpack_e4m3(uint16_t w, float& lo, float& hi) {
   uint32_t h;
@@ -224,6 +229,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const View c, co
                            pack_e4m3(bf16_lo(y.z) * inv, bf16_hi(y.z) * inv, bf16_lo(y.w) * inv, bf16_hi(y.w) * inv),
                            pack_e4m3(bf16_lo(z.x) * inv, bf16_hi(z.x) * inv, bf16_lo(z.y) * inv, bf16_hi(z.y) * inv),
                            pack_e4m3(bf16_lo(z.z) * inv, bf16_hi(z.z) * inv, bf16_lo(z.w) * inv, bf16_hi(z.w) * inv));
+      if (s == kScaleTop) codes = make_uint4(below_256(codes.x), below_256(codes.y), below_256(codes.z), below_256(codes.w));
       *reinterpret_cast<uint4*>(pages + at) = codes;
       if (lane == 0) (t ? c.v_scales : c.k_scales)[scale_at(c, page, slot, head)] = (uint8_t)s;
     }
