@@ -81,7 +81,7 @@ class PagedCache:
       k_pages, v_pages    [num_pages, page_size, kv_heads, head_dim], bfloat16 or float8_e4m3fn, alike in their strides; head_dim
                           contiguous, the other dimensions in any order (views of one tensor are fine)
       k_scales, v_scales  [num_pages, kv_heads, page_size] uint8, contiguous; e4m3 only
-      block_table         [sequences, max_pages] int32
+      block_table         [sequences, max_pages] int32, rows that do not overlap
       lengths             [sequences] int32: positions held, before the chunk of the round
     """
 
@@ -96,6 +96,8 @@ class PagedCache:
         pages, size, heads, dim = k_pages.shape
         _expect(block_table.dim() == 2 and block_table.dtype == torch.int32 and (block_table.stride(1) == 1 or block_table.size(1) == 1),
                 "block_table is [sequences, max_pages] int32 with contiguous rows")
+        _expect(block_table.size(0) == 1 or block_table.stride(0) >= block_table.size(1),
+                "rows of block_table do not overlap (an expanded one: .contiguous())")
         _expect(lengths.dtype == torch.int32 and tuple(lengths.shape) == (block_table.size(0),) and lengths.is_contiguous(),
                 "lengths is [sequences] int32")
         _expect(e4m3 == (k_scales is not None) == (v_scales is not None), "k_scales and v_scales belong to e4m3 pages, and to them only")
