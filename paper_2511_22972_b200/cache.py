@@ -75,6 +75,11 @@ def _expect(ok: bool, what: str):
         raise ValueError(what)
 
 
+class _Held(C.Structure):
+    """A fly_cache_t that is replaced as a whole by one assignment."""
+    _fields_ = [("c", fly_cache_t)]
+
+
 class PagedCache:
     """A cache over the caller's tensors (kept, not copied):
 
@@ -83,6 +88,9 @@ class PagedCache:
       k_scales, v_scales  [num_pages, kv_heads, page_size] uint8, contiguous; e4m3 only
       block_table         [sequences, max_pages] int32, rows that do not overlap
       lengths             [sequences] int32: positions held, before the chunk of the round
+
+    block_table and lengths can be assigned: calls from then on use the new tensor (a table may be wider than the one before, but is for
+    as many sequences).  The others are fixed.  Tensors keep their storage while the cache has them (no resize_, no set_).
     """
 
     def __init__(self, k_pages, v_pages, block_table, lengths, k_scales=None, v_scales=None):
@@ -94,26 +102,66 @@ class PagedCache:
         _expect(v_pages.dtype == k_pages.dtype and v_pages.shape == k_pages.shape and v_pages.stride() == k_pages.stride(),
                 "k_pages and v_pages are alike in type, shape and strides")
         pages, size, heads, dim = k_pages.shape
-        _expect(block_table.dim() == 2 and block_table.dtype == torch.int32 and (block_table.stride(1) == 1 or block_table.size(1) == 1),
-                "block_table is [sequences, max_pages] int32 with contiguous rows")
-        _expect(block_table.size(0) == 1 or block_table.stride(0) >= block_table.size(1),
-                "rows of block_table do not overlap (an expanded one: .contiguous())")
-        _expect(lengths.dtype == torch.int32 and tuple(lengths.shape) == (block_table.size(0),) and lengths.is_contiguous(),
-                "lengths is [sequences] int32")
+        self._check_table(block_table)
+        self._check_lengths(lengths, block_table)
         _expect(e4m3 == (k_scales is not None) == (v_scales is not None), "k_scales and v_scales belong to e4m3 pages, and to them only")
         for s in (k_scales, v_scales) if e4m3 else ():
             _expect(s.dtype == torch.uint8 and tuple(s.shape) == (pages, heads, size) and s.is_contiguous(),
                     "scales are [num_pages, kv_heads, page_size] uint8, contiguous")
         tensors = [t for t in (k_pages, v_pages, block_table, lengths, k_scales, v_scales) if t is not None]
         _expect(all(t.is_cuda and t.device == k_pages.device for t in tensors), "all tensors of a cache are on one CUDA device")
-        self.k_pages, self.v_pages, self.k_scales, self.v_scales = k_pages, v_pages, k_scales, v_scales
-        self.block_table, self.lengths = block_table, lengths
+        self._pages = k_pages, v_pages, k_scales, v_scales
+        self._held = _Held()
+        self._at = C.addressof(self._held)
+        self._set(block_table, lengths)
+
+    @staticmethod
+    def _check_table(t):
+        import torch
+        _expect(isinstance(t, torch.Tensor) and t.dim() == 2 and t.dtype == torch.int32 and (t.stride(1) == 1 or t.size(1) == 1),
+                "block_table is [sequences, max_pages] int32 with contiguous rows")
+        _expect(t.size(0) == 1 or t.stride(0) >= t.size(1), "rows of block_table do not overlap (an expanded one: .contiguous())")
+
+    @staticmethod
+    def _check_lengths(t, table):
+        import torch
+        _expect(isinstance(t, torch.Tensor) and t.dtype == torch.int32 and tuple(t.shape) == (table.size(0),) and t.is_contiguous(),
+                "lengths is [sequences] int32")
+
+    def _set(self, table, lengths):
+        k, v, ks, vs = self._pages
         address = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-        self.struct = fly_cache_t(k_pages.device.index, FLY_CACHE_E4M3 if e4m3 else FLY_CACHE_BF16, address(k_pages), address(v_pages),
-                                  address(k_scales), address(v_scales), pages, size, heads, dim, k_pages.stride(0), k_pages.stride(1),
-                                  k_pages.stride(2), address(block_table), max(block_table.stride(0), block_table.size(1)),
-                                  block_table.size(1), block_table.size(0), address(lengths))
-        self._at = C.addressof(self.struct)
+        self._held.c = fly_cache_t(k.device.index, FLY_CACHE_BF16 if ks is None else FLY_CACHE_E4M3, address(k), address(v), address(ks), address(vs),
+                                   *k.shape, k.stride(0), k.stride(1), k.stride(2), address(table), max(table.stride(0), table.size(1)),
+                                   table.size(1), table.size(0), address(lengths))
+        self._block_table, self._lengths = table, lengths
+
+    k_pages = property(lambda self: self._pages[0])
+    v_pages = property(lambda self: self._pages[1])
+    k_scales = property(lambda self: self._pages[2])
+    v_scales = property(lambda self: self._pages[3])
+    struct = property(lambda self: self._held.c, doc="The fly_cache_t of the calls.")
+
+    @property
+    def block_table(self):
+        return self._block_table
+
+    @block_table.setter
+    def block_table(self, t):
+        self._check_table(t)
+        _expect(t.size(0) == self._lengths.size(0), "block_table is for as many sequences as lengths")
+        _expect(t.device == self.k_pages.device, "all tensors of a cache are on one CUDA device")
+        self._set(t, self._lengths)
+
+    @property
+    def lengths(self):
+        return self._lengths
+
+    @lengths.setter
+    def lengths(self, t):
+        self._check_lengths(t, self._block_table)
+        _expect(t.device == self.k_pages.device, "all tensors of a cache are on one CUDA device")
+        self._set(self._block_table, t)
 
 
 def cache_append(cache: PagedCache, k, v, counts=None, row_flags=None, stream: int = 0):

@@ -420,6 +420,7 @@ PyObject* py_cache_append(PyObject*, PyObject* const* v, Py_ssize_t n) {
   if (!enough(n, 6)) return nullptr;
   const fly_cache_t* c = (const fly_cache_t*)PyLong_AsVoidPtr(v[0]);
   if (!c) return PyErr_Occurred() ? nullptr : status(FLY_ERR_INVALID_ARG);
+  const fly_cache_t cache = *c;  // (another thread may give the cache other tensors while the call is under way)
   int64_t B = -1, m = -1;
   fly_rows_t k, w;
   void *counts, *flags;
@@ -432,7 +433,7 @@ PyObject* py_cache_append(PyObject*, PyObject* const* v, Py_ssize_t n) {
   fly_status_t s;
   {
     Unlocked unlocked;
-    s = api.cache_append(c, (int32_t)B, (int32_t)m, &k, &w, (const int32_t*)counts, (uint32_t*)flags, stream);
+    s = api.cache_append(&cache, (int32_t)B, (int32_t)m, &k, &w, (const int32_t*)counts, (uint32_t*)flags, stream);
   }
   return status(s);
 }
@@ -442,6 +443,7 @@ PyObject* py_cache_read(PyObject*, PyObject* const* v, Py_ssize_t n) {
   if (!enough(n, 5)) return nullptr;
   const fly_cache_t* c = (const fly_cache_t*)PyLong_AsVoidPtr(v[0]);
   if (!c) return PyErr_Occurred() ? nullptr : status(FLY_ERR_INVALID_ARG);
+  const fly_cache_t cache = *c;  // (another thread may give the cache other tensors while the call is under way)
   int64_t B = -1, m = -1;
   fly_rows_t k, w;
   void* starts;
@@ -453,7 +455,7 @@ PyObject* py_cache_read(PyObject*, PyObject* const* v, Py_ssize_t n) {
   fly_status_t s;
   {
     Unlocked unlocked;
-    s = api.cache_read(c, (int32_t)B, (int32_t)m, (const int32_t*)starts, &k, &w, stream);
+    s = api.cache_read(&cache, (int32_t)B, (int32_t)m, (const int32_t*)starts, &k, &w, stream);
   }
   return status(s);
 }
@@ -465,6 +467,7 @@ PyObject* py_attention_run(PyObject*, PyObject* const* v, Py_ssize_t n) {
   if (!h && PyErr_Occurred()) return nullptr;
   const fly_cache_t* c = (const fly_cache_t*)PyLong_AsVoidPtr(v[1]);
   if (!c) return PyErr_Occurred() ? nullptr : status(FLY_ERR_INVALID_ARG);
+  const fly_cache_t cache = *c;
   int64_t B = -1, m = -1;
   long long heads, window, sinks;
   fly_attention_args_t a = {};
@@ -483,7 +486,7 @@ PyObject* py_attention_run(PyObject*, PyObject* const* v, Py_ssize_t n) {
   fly_status_t s;
   {
     Unlocked unlocked;
-    s = api.attention_run(h, c, &a, stream);
+    s = api.attention_run(h, &cache, &a, stream);
   }
   return status(s);
 }
