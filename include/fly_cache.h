@@ -15,6 +15,8 @@
  *     host can see is refused with a return code before anything is launched.  lengths, counts, starts and block_table are device data:
  *     no value in them makes a call read or write outside the cache and the caller's buffers (what each bad one does stands
  *     beside it).
+ *     They must not change until the step that was given them has ended; if they do, its results mean nothing, but it ends
+ *     (attention: with FLY_ERR_TIMEOUT from fly_attention_device_status where its parts no longer agreed on what to do).
  *   - Position p of sequence b is slot p % page_size of page block_table[b][p / page_size].
  *   - The chunk of sequence b starts at position lengths[b]: lengths is what the cache held BEFORE the chunk, in all calls.
  *     lengths[b] has to lie in [0, max_pages * page_size]; another one counts as a sequence without any position: nothing

@@ -253,7 +253,7 @@ struct Shape {
   static constexpr int kOffScales = kOffRaw + kRawStages * kRawBytes;
   static constexpr int kOffExchange = kOffScales + (E4M3 ? kScaleRing * kTile * 4 + kKStages * kTile : 0);  // fp32, bytes by stage
   static constexpr int kOffBar = kOffExchange + 2 * kTileRows * 8;
-  static constexpr int kNumBars = 3 * kKStages + 2 * kVStages + 2 * kRawStages + 4 + 6 + 1;
+  static constexpr int kNumBars = 3 * kKStages + 2 * kVStages + 2 * kRawStages + 4 + 6 + 2;
   static constexpr int kOffFlags = kOffBar + kNumBars * 8;
   static constexpr int kOffMisc = kOffFlags + 2 * 16 * 4;
   static constexpr int kSmem = kOffMisc + 64;
@@ -643,7 +643,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
   auto raw_empty = [&](uint32_t s) { return bar0 + 8u * (2 * S::kKStages + 2 * S::kVStages + S::kRawStages + s); };
   constexpr uint32_t kB = 2 * S::kKStages + 2 * S::kVStages + 2 * S::kRawStages, kRaw = E4M3 ? S::kRawStages : 1;
   auto k_ready = [&](uint32_t s) { return E4M3 ? bar0 + 8u * (kB + 10 + s) : k_full(s); };  // ... and for E4M3 its keys' scales are in fp32
-  const uint32_t drained = bar0 + 8u * (S::kNumBars - 1);                  // (after a wait has run out) no MMA is in flight
+  const uint32_t drained = bar0 + 8u * (S::kNumBars - 1);                  // no MMA is in flight
+  const uint32_t met = bar0 + 8u * (S::kNumBars - 2);                      // all warps of the two slots of one row tile are there
   auto q_full = [&](int s) { return bar0 + 8u * (kB + s); };
   auto q_empty = [&](int s) { return bar0 + 8u * (kB + 2 + s); };
   auto s_full = [&](int s) { return bar0 + 8u * (kB + 4 + s); };          // S of a slot's step is complete (and every MMA before it)
@@ -675,6 +676,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       mbar_init(o_full(s), 1);
     }
     mbar_init(drained, 1);
+    mbar_init(met, 2 * kTileRows / 32);
     misc[1] = 0;
     for (int i = 8; i < 16; ++i) misc[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -795,6 +797,12 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       if (failed) break;
       tile_no += m;
     }
+    // The last tiles have arrived before this warp lets the CTA end, whether or not somebody has taken them.
+    const uint32_t stages = !values ? S::kKStages : E4M3 ? kRaw : S::kVStages;
+    for (uint32_t no = tile_no > stages ? tile_no - stages : 0u; no < tile_no; ++no) {
+      const uint32_t st = no % stages;
+      wait_warp(!values ? k_full(st) : E4M3 ? raw_full(st) : v_full(st), (no / stages) & 1);
+    }
   } else if (warp == S::kWarpQ) {
     // ---------------- queries: (heads of the group, tokens) boxes; tokens behind the chunk's end come as zeros ----------------
     // E4M3: the softmax warps take the queries apart themselves, and this one turns the keys' scale bytes into fp32, four a lane.
@@ -825,6 +833,10 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         }
         __syncwarp();
       }
+    }
+    for (int s = 0; s < (E4M3 ? 0 : 2); ++s) {  // (as above: the last use of each buffer)
+      const uint32_t uses = PAIR ? item : (item + 1u - (uint32_t)s) / 2u;
+      if (uses > 0) wait_warp(q_full(s), (uses - 1u) & 1);
     }
     // ... and the rows of sequences that hold no position at all
     for (int64_t g = blockIdx.x + (int64_t)gridDim.x * lane; g < p.groups; g += (int64_t)gridDim.x * 32) {
@@ -967,9 +979,11 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       }
       tile_no += m;
     }
-    if (failed && issued) {  // what has been issued ends before shared and tensor memory are given back
+    if (issued) {  // what has been issued ends before shared and tensor memory are given back, whatever the other warps have waited for
       if (lead) mma_commit(drained);
-      mbar_wait_quiet(drained, 0, 2000000ull);
+      __syncwarp();
+      if (failed) mbar_wait_quiet(drained, 0, 2000000ull);
+      else wait_warp(drained, 0);
     }
     __syncwarp();
   }
@@ -1046,7 +1060,14 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const uint32_t ts = tmem + lanes + slot * kTile, to = tmem + lanes + 2 * kTile + slot * 128;
     const int row_token = row / p.group, row_head = row - row_token * p.group;
-    uint32_t use = 0, items_done = 0, item = 0;
+    uint32_t use = 0, items_done = 0, item = 0, meetings = 0;
+    // (A barrier with a bounded wait, not bar.sync: should lengths change during the step, the warps may not agree on how many items there are.
+    // A warp that has given up does not arrive, so that the others do not go on without it.)
+    auto meet = [&]() {
+      __syncwarp();
+      if (!failed && lane == 0) mbar_arrive(met);
+      wait_warp(met, meetings++ & 1);
+    };
     for (; walk.have(); walk.next(), ++item) {
       const Group& g = walk.gr;
       const int m = walk.tiles();
@@ -1078,7 +1099,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         uint32_t amax = max(m2 & 0xffffu, m2 >> 16);
         if (!PAIR) {
           exchange[slot * kTileRows + row].x = __uint_as_float(amax);
-          asm volatile("bar.sync 1, 256;" ::: "memory");
+          meet();
           amax = max(amax, __float_as_uint(exchange[(slot ^ 1) * kTileRows + row].x));
         }
         const int s = cache::scale_of(amax);
@@ -1102,7 +1123,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         }
         async_proxy_fence();
         if (!failed) mbar_arrive(q_full(PAIR ? slot : 0));
-        if (!PAIR) asm volatile("bar.sync 1, 256;" ::: "memory");  // (the exchange is used again at the item's end)
+        if (!PAIR) meet();  // (the exchange is used again at the item's end)
       }
       for (int j = PAIR ? 0 : slot; j < m; j += PAIR ? 1 : 2) {
         const int p0 = tile_start(g, walk.x0 + j);
@@ -1180,7 +1201,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       bool use0 = PAIR ? begun : true, use1 = false;  // whether there is an O of each slot
       if (!PAIR) {
         exchange[slot * kTileRows + row] = make_float2(ref, failed ? quiet_nan() : sum);  // (the other slot's columns are NaN too)
-        asm volatile("bar.sync 1, 256;" ::: "memory");  // both slots' O are complete as well
+        meet();  // both slots' O are complete as well
         const float2 a = exchange[row], b = exchange[kTileRows + row];
         use1 = m > 1;
         r = fmaxf(a.x, use1 ? b.x : -INFINITY);
@@ -1245,7 +1266,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         }
         tc_fence_before();
       }
-      if (!PAIR) asm volatile("bar.sync 1, 256;" ::: "memory");  // neither slot's O is overwritten before both have read it
+      if (!PAIR) meet();  // neither slot's O is overwritten before both have read it
       tile_no += m;
     }
   }
