@@ -130,7 +130,8 @@ typedef struct {
 fly_status_t fly_attention_run(fly_attention_t* handle, const fly_cache_t* cache, const fly_attention_args_t* args,
                                void* cuda_stream);
 
-/* The kernel waits on hardware barriers (loads, tensor cores); every such wait is bounded (200 ms).  If one runs out, the kernel
+/* The kernel waits on hardware barriers (loads, tensor cores); every such wait is bounded (200 ms without a step forward of the
+ * block, however long a context is).  If one runs out, the kernel
  * records it and returns without hanging, and rows that it could not form are NaN (out and lse).  This call synchronises
  * `cuda_stream` and returns FLY_ERR_TIMEOUT if that happened since the last call (the record is cleared), else FLY_OK.  While
  * a record is pending, every further step of the handle comes back as NaN. */

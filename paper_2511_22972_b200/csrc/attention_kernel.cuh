@@ -32,8 +32,9 @@
 // values that no row sees are therefore zeroed in shared memory, and infinities and NaN in those that only some rows see are zeroed too
 // and added back to the rows that do see them (add_back).
 //
-// Every wait is bounded: one that runs out records a code in *status, after which no wait waits, the rows of the step become NaN, and the
-// CTA ends as usual.  No TMA load is a multicast load.
+// Every wait is bounded: its limit counts while the products of no further tile are issued (the next items' queries, and a slot of a pair
+// that has had an item without rows, wait for as long as an item takes).  One that runs out records a code in *status, after which no
+// wait waits, the rows of the step become NaN, and the CTA ends as usual.  No TMA load is a multicast load.
 //
 // What bounds it, and measured (1.9 GHz; us a call in a CUDA graph):
 //   long bf16 contexts, few rows   bytes: 64 sequences of one token, 64 heads over 8 of 128, 500 - 8000 positions (1.1 GB) 183 - 200, 5.6 - 6.1 TB/s
@@ -650,7 +651,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
   auto s_full = [&](int s) { return bar0 + 8u * (kB + 4 + s); };          // S of a slot's step is complete (and every MMA before it)
   auto p_ready = [&](int s) { return bar0 + 8u * (kB + 6 + s); };         // its P is there, O rescaled, the values' tile cleaned
   auto o_full = [&](int s) { return bar0 + 8u * (kB + 8 + s); };          // the slot's O of an item is complete
-  volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(smem + S::kOffMisc);  // [0] tensor memory, [1] a role gave up, [8..15] items with values to add back
+  volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(smem + S::kOffMisc);  // [0] tensor memory, [1] a role gave up, [2] tiles whose products are issued, [8..15] items with values to add back
   volatile uint32_t* tile_bad = reinterpret_cast<volatile uint32_t*>(smem + S::kOffFlags);  // of tile number t: entry t % 16, for the conversion 16 + t % 16
   float* key_scales = reinterpret_cast<float*>(smem + S::kOffScales);  // of tile number t: entry t % kScaleRing
   uint8_t* key_bytes = smem + S::kOffScales + S::kScaleRing * kTile * 4;
@@ -677,7 +678,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     }
     mbar_init(drained, 1);
     mbar_init(met, 2 * kTileRows / 32);
-    misc[1] = 0;
+    misc[1] = misc[2] = 0;
     for (int i = 8; i < 16; ++i) misc[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -714,7 +715,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
   const bool pending = __shfl_sync(0xffffffffu, lane == 0 ? *reinterpret_cast<volatile int*>(p.status) : 0, 0) != 0;
   bool failed = pending;
   auto wait_warp = [&](uint32_t bar, uint32_t parity) {  // the same decision in the whole warp
-    if (!failed && !__all_sync(0xffffffffu, mbar_wait_suspended(bar, parity, p.status, kErrAttention))) failed = true;
+    if (!failed && !__all_sync(0xffffffffu, mbar_wait_suspended(bar, parity, p.status, kErrAttention, &misc[2]))) failed = true;
   };
   const Range range = range_of(p);
   Walk walk(p, range);
@@ -924,7 +925,10 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         __syncwarp();
       };
       auto release_k = [&](int j) { commit(k_empty((tile_no + (uint32_t)j) % S::kKStages)); };
-      auto release_v = [&](int j) { commit(v_empty((tile_no + (uint32_t)j) % S::kVStages)); };
+      auto release_v = [&](int j) {
+        if (lane == 0) misc[2] = tile_no + (uint32_t)j + 1u;  // (what keeps other warps' waits from running out)
+        commit(v_empty((tile_no + (uint32_t)j) % S::kVStages));
+      };
       if (PAIR) {
         int last[2];
         for (int s = 0; s < 2; ++s) {

@@ -58,9 +58,11 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, int* st
   return true;
 }
 
-// The same wait by warps that share their scheduler with others that compute: suspended up to 20 us at a time instead of polling.
-__device__ __forceinline__ bool mbar_wait_suspended(uint32_t bar, uint32_t parity, int* status, int code) {
+// The same wait by warps that share their scheduler with others that compute: suspended up to 20 us at a time instead of polling.  The limit
+// counts from when *progress (shared memory: how far the block's work has come) last changed, for waits that rightly last as long as many steps of others.
+__device__ __forceinline__ bool mbar_wait_suspended(uint32_t bar, uint32_t parity, int* status, int code, const volatile uint32_t* progress) {
   unsigned long long t0 = 0;
+  uint32_t seen = 0;
   while (true) {
     uint32_t ok;
     asm volatile(
@@ -73,7 +75,11 @@ __device__ __forceinline__ bool mbar_wait_suspended(uint32_t bar, uint32_t parit
     if (ok) return true;
     if (*(volatile int*)status != 0) return false;
     const unsigned long long t = global_ns();
-    if (t0 == 0) t0 = t;
+    const uint32_t now = *progress;
+    if (t0 == 0 || now != seen) {
+      t0 = t;
+      seen = now;
+    }
     if (t - t0 > kWaitLimitNs) {
       atomicCAS(status, 0, code);
       return false;
