@@ -60,23 +60,27 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, int* st
 
 // The same wait by warps that share their scheduler with others that compute: suspended up to 20 us at a time instead of polling.  The limit
 // counts from when *progress (shared memory: how far the block's work has come) last changed, for waits that rightly last as long as many steps of others.
-__device__ __forceinline__ bool mbar_wait_suspended(uint32_t bar, uint32_t parity, int* status, int code, const volatile uint32_t* progress) {
-  unsigned long long t0 = 0;
-  uint32_t seen = 0;
-  while (true) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2, %3;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity), "r"(20000)
-        : "memory");
-    if (ok) return true;
-    if (*(volatile int*)status != 0) return false;
+// Out of line but for the first look: it stands in many places of a kernel whose code is larger than what an SM keeps of it (us a call in line and so:
+// window of one token over e4m3 32.8 and 29.9, 16 sequences of nine 149 and 144, 9 tokens over 300 positions 10.7 and 10.2).
+__device__ __forceinline__ bool mbar_try_wait_suspended(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity), "r"(20000)
+      : "memory");
+  return ok != 0;
+}
+static __device__ __noinline__ bool mbar_wait_on(uint32_t bar, uint32_t parity, int* status, int code, const volatile uint32_t* progress) {
+  unsigned long long t0 = global_ns();
+  uint32_t seen = *progress;
+  while (*(volatile int*)status == 0) {
+    if (mbar_try_wait_suspended(bar, parity)) return true;
     const unsigned long long t = global_ns();
     const uint32_t now = *progress;
-    if (t0 == 0 || now != seen) {
+    if (now != seen) {
       t0 = t;
       seen = now;
     }
@@ -85,6 +89,10 @@ __device__ __forceinline__ bool mbar_wait_suspended(uint32_t bar, uint32_t parit
       return false;
     }
   }
+  return false;
+}
+__device__ __forceinline__ bool mbar_wait_suspended(uint32_t bar, uint32_t parity, int* status, int code, const volatile uint32_t* progress) {
+  return mbar_try_wait_suspended(bar, parity) || mbar_wait_on(bar, parity, status, code, progress);
 }
 
 // The same wait without a status word: for the give-up path, where the failure is already recorded.
