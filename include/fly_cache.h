@@ -22,7 +22,7 @@
  *     lengths[b] has to lie in [0, max_pages * page_size]; another one counts as a sequence without any position: nothing
  *     is written or read for it, and its chunk sees nothing.
  *   - counts (dev [B] or NULL): the tokens of the chunk that sequence b really has, 0 .. n (another value counts as 0); NULL = n for all.
- *     Rows of a chunk from counts[b] on are neither read nor written.
+ *     Rows of a chunk from counts[b] on are not written and have no influence, whatever they hold (attention may read its queries there).
  */
 #ifndef FLY_CACHE_H_
 #define FLY_CACHE_H_
@@ -93,8 +93,8 @@ fly_status_t fly_cache_read(const fly_cache_t* cache, int32_t B, int32_t n, cons
  *   s_p = scale * <q, k_p>,   lse = ln sum_p e^{s_p},   out = sum_p e^{s_p - lse} v_p.
  * A row that sees nothing, or only scores of -inf, gets out 0 and lse -inf.  Keys and values that a row does not see have no
  * influence on it, whatever they hold.  Products are added up in fp32 (weights rounded to bf16; over E4M3 a query is
- * exact down to 2^-17 of the largest of its row and off by 2^-22 of that below), so magnitudes beyond 2^100 may overflow on the way, and
- * a row with scores beyond 2^30, of whose weights fp32 leaves nothing, may come out as NaN.
+ * exact down to 2^-13.8 of the largest of its row and off by at most 2^-21.8 of that, or 2^-134, below), so magnitudes beyond 2^100 may
+ * overflow on the way, and a row with scores beyond 2^30, of whose weights fp32 leaves nothing, may come out as NaN.
  * out may be q itself; otherwise the two do not overlap.
  *
  * A handle owns the scratch in which the parts of a long context meet, so steps of one handle run one after the other

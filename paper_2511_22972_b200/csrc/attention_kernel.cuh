@@ -20,8 +20,9 @@
 // attention_combine_kernel adds them up, in a fixed order.
 //
 // E4M3.  The first product takes the keys' codes as they are (kind::f8f6f4) and the queries as the sum of an e4m3 and an e5m2 part: a bf16
-// has eight significant bits, four in the first part and what is left in at most three of the second, so a row scaled to the range
-// of e4m3 is exact down to 2^-17 of its largest value and off by 2^-22 of that below.  A token's key scale multiplies its column of
+// has eight significant bits, four in the first part and what is left in at most three of the second.  So a row that is scaled to have its
+// largest value in 224 .. 448 is exact down to 2^-6, where e4m3's normal numbers end: 2^-13.8 of the largest.  Below, up to 2^-10 is left for
+// three bits: off by at most 2^-14, 2^-21.8 of the largest (every bf16 number tried).  A token's key scale multiplies its column of
 // scores.  The values' codes become tiles of bf16 (exactly: a code times a power of two is a bf16 number), since weights cover far more
 // binades than 8 bits do.
 //

@@ -14,7 +14,6 @@ namespace fly {
 namespace cache {
 
 constexpr uint32_t kFlagNotWritten = 32u;  // row_flags bit 5
-constexpr int kScaleBias = 127;
 constexpr int kScaleMin = 7;               // 2^-120: what is held stays exact in bf16
 constexpr int kScaleTop = 247;             // of the largest bf16 numbers: codes from 256 on are not finite
 constexpr int kScaleNan = 255;
