@@ -98,14 +98,11 @@ K::View view_of(const fly_cache_t* c) {
 
 K::Rows rows_of(const fly_rows_t* r) { return {static_cast<uint8_t*>(r->data), r->batch_stride, r->token_stride, r->head_stride}; }
 
-// Groups of head_dim / 16 threads with one or `at_once` rows (tokens x heads) each, sequences along y.  Several rows at once where that still leaves
-// every SM its eight blocks.
-bool row_grid(const fly_cache_t* c, int32_t B, int32_t n, int threads, int at_once, dim3* grid, bool* several) {
-  const int64_t per_block = threads / (c->head_dim / 16), rows = (int64_t)n * c->kv_heads;
+// Groups of head_dim / 16 threads with `each` rows (tokens x heads) to a group, sequences along y.
+bool row_grid(const fly_cache_t* c, int32_t B, int32_t n, int threads, int each, dim3* grid) {
+  const int64_t per_block = (int64_t)(threads / (c->head_dim / 16)) * each, rows = (int64_t)n * c->kv_heads;
   if (rows > 0x7fffff00) return false;  // (rows of a sequence are counted in 32 bits)
-  *several = at_once > 1 && (rows * B) / (per_block * at_once) >= 148 * 8;
-  const int64_t each = per_block * (*several ? at_once : 1);
-  *grid = dim3((unsigned)((rows + each - 1) / each), (unsigned)(B < 65535 ? B : 65535));
+  *grid = dim3((unsigned)((rows + per_block - 1) / per_block), (unsigned)(B < 65535 ? B : 65535));
   return true;
 }
 
@@ -191,8 +188,7 @@ fly_status_t fly_cache_append(const fly_cache_t* c, int32_t B, int32_t n, const 
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute attr[1];
   fill_launch(&cfg, attr, 1, K::kAppendThreads, static_cast<cudaStream_t>(cuda_stream), true);
-  bool several;
-  if (!row_grid(c, B, n, K::kAppendThreads, 1, &cfg.gridDim, &several)) return FLY_ERR_UNSUPPORTED;
+  if (!row_grid(c, B, n, K::kAppendThreads, 1, &cfg.gridDim)) return FLY_ERR_UNSUPPORTED;
   const bool e4m3 = c->format == FLY_CACHE_E4M3;
   auto kernel = c->head_dim == 128 ? (e4m3 ? K::append_kernel<128, true> : K::append_kernel<128, false>)
                                    : (e4m3 ? K::append_kernel<64, true> : K::append_kernel<64, false>);
@@ -212,10 +208,14 @@ fly_status_t fly_cache_read(const fly_cache_t* c, int32_t B, int32_t n, const in
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute attr[1];
   fill_launch(&cfg, attr, 1, K::kReadThreads, static_cast<cudaStream_t>(cuda_stream), true);
-  bool several;
-  if (!row_grid(c, B, n, K::kReadThreads, K::kReadRows, &cfg.gridDim, &several)) return FLY_ERR_UNSUPPORTED;
-  const bool e4m3 = c->format == FLY_CACHE_E4M3;
+  if (!row_grid(c, B, n, K::kReadThreads, 1, &cfg.gridDim)) return FLY_ERR_UNSUPPORTED;
+  // Several rows to a group where that still leaves every SM its eight blocks.
   constexpr int R = K::kReadRows;
+  int sms = 0;
+  if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, c->device) != cudaSuccess) return FLY_ERR_CUDA;
+  const bool several = (int64_t)n * c->kv_heads * B / (K::kReadThreads / (c->head_dim / 16) * R) >= sms * 8;
+  if (several && !row_grid(c, B, n, K::kReadThreads, R, &cfg.gridDim)) return FLY_ERR_UNSUPPORTED;
+  const bool e4m3 = c->format == FLY_CACHE_E4M3;
   auto kernel = c->head_dim == 128 ? (e4m3 ? (several ? K::read_kernel<128, true, R> : K::read_kernel<128, true, 1>)
                                            : (several ? K::read_kernel<128, false, R> : K::read_kernel<128, false, 1>))
                                    : (e4m3 ? (several ? K::read_kernel<64, true, R> : K::read_kernel<64, true, 1>)
