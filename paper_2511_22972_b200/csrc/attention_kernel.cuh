@@ -38,10 +38,12 @@
 // wait waits, the rows of the step become NaN, and the CTA ends as usual.  No TMA load is a multicast load.
 //
 // What bounds it, and measured (1.9 GHz; us a call in a CUDA graph):
-//   long bf16 contexts, few rows   bytes: 64 sequences of one token, 64 heads over 8 of 128, 500 - 8000 positions (1.1 GB) 183 - 200, 5.6 - 6.1 TB/s
-//   chunks of 2000 over 4 - 8 k    the softmax: two slots of 2200 cycles a tile, exponentials and tensor pipe at 48 % each; 980 = 0.93 PFLOP/s
-//   E4M3                           turning values' codes into bf16, 3400 cycles a tile: 16 sequences of nine, 2 - 16 k positions 139, 2.2 TB/s
-//   short contexts                 latency: start and schedule 4 us, a tile 3, the end 2; 9 tokens over 300 positions 10.1
+//   long bf16 contexts, few rows   bytes: 64 sequences of one token, 64 heads over 8 of 128, 500 - 8000 positions (1.1 GB) 184 - 200, 5.6 - 6.1 TB/s,
+//                                  for the first 50 ms; in loops of a second (1 kW, 1.6 GHz) 202 - 217
+//   chunks of 2000 over 4 - 8 k    the softmax: two slots of 2200 cycles a tile, exponentials and tensor pipe at 48 % each; 976 - 1010 = 0.91 - 0.94 PFLOP/s
+//   E4M3                           turning values' codes into bf16, 3400 cycles a tile: 16 sequences of nine, 2 - 16 k positions 137 - 149, 2.0 - 2.2 TB/s
+//   short contexts                 latency: start and schedule 4 us, a tile 3, the end 2; 9 tokens over 300 positions 10.0
+//   a context over many SMs        its parts: 16 tokens over 30000 positions 38, of which the kernel that adds up takes 9
 #pragma once
 #include <cuda.h>
 
