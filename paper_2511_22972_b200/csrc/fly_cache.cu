@@ -313,6 +313,7 @@ fly_status_t fly_attention_run(fly_attention_t* h, const fly_cache_t* c, const f
   // (tiles of positions are counted in 32 bits, lengths are not known here)
   // What an item takes besides its tiles, in tiles (its queries, the joining of the slots, its end).  us a call at 0 / 2 / 4: 64 sequences of one token
   // 222 / 193 / 191, 16 of nine over e4m3 169 / 158 / 147, window of one token over e4m3 36.4 / 32.6 / 34.7 (3 for e4m3: 151 and 33.0).
+  // (193 and 191 are as good as equal: repeated runs differ by 1 % and more.)
   const int item_cost = c->format == FLY_CACHE_E4M3 ? 3 : 2;
   if (groups > 1 << 28 || groups * kv_heads * ((int64_t)p.c.capacity / A::kTile + 2 + item_cost) > 0x7fffffff) return FLY_ERR_UNSUPPORTED;
   p.groups = (int)groups;
